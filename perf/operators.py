@@ -164,7 +164,7 @@ def prepare(case, seed):
             s["acc"] = torch.exp(2 * normal(hk, total)) * (torch.rand(hk, total, generator=g, device="cuda") > 0.05)
             s["slot_pos"] = torch.zeros(len(lens), hk, case["capacity"], dtype=torch.int32, device="cuda")
             s["slot_acc"] = torch.zeros(len(lens), hk, case["capacity"], device="cuda")
-            s["length"] = torch.zeros(len(lens), dtype=torch.int32, device="cuda")
+            s["length"] = torch.zeros(len(lens), hk, dtype=torch.int32, device="cuda")
             s["cache"] = torch.zeros(sum(_sections(len(lens), hk, d, case["capacity"])), dtype=torch.uint8, device="cuda")
             s["k_rows"], s["v_rows"] = (torch.zeros(len(lens), hk, case["capacity"], d, dtype=dt, device="cuda") for _ in range(2))
         return s
@@ -182,7 +182,7 @@ def prepare(case, seed):
     s["slot_pos"] = torch.where(torch.rand(b, hk, c, generator=g, device="cuda") < case["fill"], pos, -1).to(torch.int32)
     s["q"], s["k_new"], s["v_new"] = ((normal(b, m, d) * f).to(dt) for m, f in ((h, 2.0), (hk, 1.0), (hk, 1.0)))
     if case["op"] == "evict_step":
-        s["length"] = n.to(torch.int32)
+        s["length"] = n.to(torch.int32).unsqueeze(1).repeat(1, hk)
         s["slot_acc"] = torch.exp(2 * normal(b, hk, c)) * (s["slot_pos"] >= 0)
         taken = torch.cat([(s["slot_pos"] >= 0).repeat_interleave(h // hk, 1), torch.ones(b, h, 1, dtype=torch.bool, device="cuda")], -1)
         s["weights"] = torch.softmax(torch.where(taken, 2 * normal(b, h, c + 1), float("-inf")), -1)
@@ -253,7 +253,7 @@ def _plain_evict_prompt(s):
                 rows = s[x][at:at + n].permute(1, 0, 2).gather(1, kept.unsqueeze(-1).expand(hk, m, d)).float()
                 to[i, :, :m] = _in_four_bits(rows).to(dt)
         at += n
-    length = s["seq_start"][1:] - s["seq_start"][:-1]
+    length = (s["seq_start"][1:] - s["seq_start"][:-1]).unsqueeze(1).repeat(1, hk)
     return dict(slot_pos=pos, slot_acc=acc, length=length, k=k_rows, v=v_rows)
 
 
@@ -264,13 +264,13 @@ def _plain_evict_step(s):
     got = s["weights"].view(b, hk, h // hk, cap + 1).double().sum(2)
     acc = torch.where(pos >= 0, (s["slot_acc"].double() + got[..., :cap]).float(), 0.0)
     free = pos < 0
-    old = (pos <= s["length"].view(b, 1, 1) - c["recent"]) & ~free
+    old = (pos <= s["length"].unsqueeze(-1) - c["recent"]) & ~free
     value = torch.where(free, -1.0, torch.where(old, acc, float("inf")))
     admit = torch.where(value == value.amin(-1, keepdim=True), slots, cap).amin(-1)
     here = slots == admit.unsqueeze(-1)
     evicted = torch.where(here, pos, 0).sum(-1).to(torch.int32)
     s["slot_acc"].copy_(torch.where(here, got[..., cap:].float(), acc))
-    s["slot_pos"].copy_(torch.where(here, s["length"].view(b, 1, 1), pos))
+    s["slot_pos"].copy_(torch.where(here, s["length"].unsqueeze(-1), pos))
     s["length"] += 1
     rows = [_in_four_bits(s[x].float()).to(s[x].dtype).unsqueeze(2) for x in ("k_new", "v_new")]
     return dict(slot_pos=s["slot_pos"], slot_acc=s["slot_acc"], length=s["length"], admit_slot=admit.to(torch.int32), evicted_pos=evicted,
@@ -391,7 +391,7 @@ def exact(case, seed):
         acc = s["slot_acc"].double()
         got = s["weights"].double().unflatten(1, (hk, h // hk)).sum(2)
         for b in range(case["batch"]):
-            n = int(s["length"][b])
+            n = int(s["length"][b, 0])
             for head in range(hk):
                 pos = s["slot_pos"][b, head].tolist()
                 a = torch.where(s["slot_pos"][b, head] >= 0, acc[b, head] + got[b, head, :-1], 0.0)

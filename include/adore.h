@@ -382,6 +382,128 @@ adore_status_t adore_cache_import_state(adore_cache_t *cache, const void *host_b
  * or CUDA if the stream itself failed). The word is cleared. */
 adore_status_t adore_cache_sync_status(adore_cache_t *cache);
 
+/* ---- Whole prompts, eviction by attention weight, rows in 4 bits --------------------------------------------------
+ *
+ * The H2O baselines (Section 3.1, items 6 and 7) keep, per head, the tokens that received most attention and the newest
+ * ones. The calls below serve that policy from the prompt on, with a slot map per key/value head:
+ *
+ *   adore_prompt_attention   causal attention of whole prompts, out and log-sum-exp of every row
+ *   adore_prompt_weights     attention weight that every prompt token received (from all queries or from the last ones)
+ *   adore_evict_prompt       keeps the C most valuable tokens per key/value head, their rows in 4 bits
+ *   adore_q4_attention       decode attention over those rows and the token's own, per-slot weights emitted
+ *   adore_evict_step         adds the step's weights, releases the least valuable token, admits the new one in 4 bits
+ *
+ * They need no cache object, allocate nothing, run on the given CUDA stream (NULL = default stream) of the current
+ * device and can be captured into a CUDA graph. All pointers are DEVICE pointers of that device. Element type T is float
+ * or bfloat16; head_dim is 64 or 128 (ADORE_ERR_UNSUPPORTED otherwise); n_heads is a multiple of n_kv_heads, and query
+ * head h uses key/value head h / (n_heads / n_kv_heads). scale multiplies the logits; 0 means 1/sqrt(head_dim).
+ *
+ * error_word: uint32 DEVICE word or NULL. Inconsistencies that only the device sees are skipped there, never followed,
+ * and leave a bit (ADORE_WORD_*) in the word; the caller clears it. */
+enum { ADORE_WORD_TIMEOUT = 1, ADORE_WORD_BOUNDS = 4 };
+
+/* Packed sequences: row t of q, k, v, out belongs to the sequence s with seq_start[s] <= t < seq_start[s + 1]. Rows
+ * outside [seq_start[0], seq_start[n_seqs]) belong to none: they are not read into any result and not written, whatever
+ * they hold. Sequences may be empty. seq_start[0] >= 0, ascending, seq_start[n_seqs] <= total: a sequence that breaks this
+ * is skipped and sets ADORE_WORD_BOUNDS. The rows of a sequence have to be finite.
+ * Strides are in elements: element (t, h, e) of q is q[t * q_row + h * q_head + e]. Every row starts on a 16-byte
+ * boundary (INVALID_ARG otherwise) and q, k, v may overlap one another (parts of one projection's output); rows of out
+ * may not overlap. */
+typedef struct {
+  uint32_t struct_size;  /* sizeof(adore_prompt_t) */
+  adore_dtype_t dtype;
+  int32_t n_seqs;        /* >= 1 */
+  int32_t total;         /* rows of the packed tensors, >= 0 */
+  int32_t n_heads, n_kv_heads, head_dim;
+  float scale;
+  int64_t q_row, q_head, k_row, k_head, v_row, v_head, out_row, out_head;
+} adore_prompt_t;
+
+/* Causal self-attention of every sequence (Section 2.1's Attention(Q, K, V) over a whole prompt):
+ *   s_ij = scale q_i . k_j for j <= i,  lse_i = log sum_j exp(s_ij),  out_i = sum_j exp(s_ij - lse_i) v_j.
+ * lse: float[n_heads, total] or NULL. Logits, softmax and sums are float32; with T = bfloat16 the weights are rounded to
+ * bfloat16 before they meet v. Errors: INVALID_ARG, UNSUPPORTED, CUDA. */
+adore_status_t adore_prompt_attention(const adore_prompt_t *shape, const int32_t *seq_start, const void *q,
+                                      const void *k, const void *v, void *out, float *lse, uint32_t *error_word,
+                                      void *cuda_stream);
+
+/* Attention weight received by every prompt token (Section 3.1, items 6 and 7: cumulative attention):
+ *   acc[g, j] = sum over the query heads of key/value head g, sum over i >= j of exp(s_ij - lse_i)
+ * with the queries i limited to the last `window` of each sequence (0: all of them). lse as adore_prompt_attention wrote
+ * it; acc: float[n_kv_heads, total]. v and out strides of the shape are ignored. The order of the sums is fixed, so the
+ * same inputs give the same bits. Errors: INVALID_ARG, UNSUPPORTED, CUDA. */
+adore_status_t adore_prompt_weights(const adore_prompt_t *shape, const int32_t *seq_start, const void *q, const void *k,
+                                    const float *lse, int32_t window, float *acc, uint32_t *error_word,
+                                    void *cuda_stream);
+
+/* A cache of C slots per (sequence b, key/value head g) whose rows are held in 4 bits. Groups of 64 elements share a step
+ * and a low value, both bfloat16: low = min, step = max(max - low, 0) / 15, code = clamp(round((x - low) / step), 0, 15)
+ * (0 where step is 0), value = code * step + low; arithmetic in float32, low and step rounded to nearest before they are
+ * used, so an element is off by at most step / 2 plus the rounding of low and step (2^-8 of their values). One buffer of
+ * adore_q4_bytes() bytes on a 16-byte boundary holds, one after the other, with P = C rounded up to a multiple of 16 and
+ * rows r = b * n_kv_heads + g:
+ *   key codes    uint32 [r][P][4][dh/32]: word (t, i) holds elements 32 i + 8 t + n at bits 4 n, n = 0..7
+ *   value codes  uint32 [r][P/2][8][dh/32]: word (t, i) holds elements 32 i + 4 t + n of slot 2 p at bits 4 n and of slot
+ *                2 p + 1 at bits 16 + 4 n, n = 0..3
+ *   key pairs    bfloat16 [r][P][dh/64][2]: step, low
+ *   value pairs  the same
+ * What empty slots hold does not matter.
+ * slot_pos: int32[batch, n_kv_heads, C], position of the token in each slot, negative where the slot is empty. */
+typedef struct {
+  uint32_t struct_size;  /* sizeof(adore_q4_t) */
+  adore_dtype_t dtype;   /* of q, k, v, out */
+  int32_t batch, n_heads, n_kv_heads, head_dim;
+  int32_t capacity;      /* C >= 1 */
+  float scale;
+} adore_q4_t;
+
+/* Bytes of the cache buffer; 0 if the shape is not supported. */
+size_t adore_q4_bytes(const adore_q4_t *shape);
+
+/* End of a prompt: fills the cache of every (sequence, key/value head) from packed rows (Section 3.1 items 6 and 7; the
+ * released rest of Section 2.1). All tokens of a sequence that has at most C, otherwise the newest `recent` (1 <= recent
+ * <= C) and, of the others, the C - recent with the largest acc (equal: lower position first; NaN counts as less than
+ * every number). Kept tokens take slots 0, 1, .. in ascending position; the slots behind them are empty, their rows zero.
+ *   rows: the packed shape (n_seqs = cache->batch; head counts, head_dim and dtype as in cache); k, v as there.
+ *   acc: float[n_kv_heads, rows->total].  cache_rows: the buffer, written whole.
+ *   slot_pos: out.  slot_acc: out, float[batch, n_kv_heads, C], acc of the kept tokens, 0 in empty slots.
+ *   length: out, int32[batch, n_kv_heads], tokens of the sequence (0 for a sequence that is skipped).
+ * Errors: INVALID_ARG, UNSUPPORTED, CUDA. */
+adore_status_t adore_evict_prompt(const adore_q4_t *cache, const adore_prompt_t *rows, const int32_t *seq_start,
+                                  const float *acc, const void *k, const void *v, int32_t recent, void *cache_rows,
+                                  int32_t *slot_pos, float *slot_acc, int32_t *length, uint32_t *error_word,
+                                  void *cuda_stream);
+
+/* After a decode step's attention (Section 2.2's release rule with the cumulative attention of Section 3.1 as the value):
+ * slot_acc of every occupied slot gains the weights of its key/value head's query heads (summed in float64, rounded once);
+ * the new token takes the lowest empty slot, or else that of the least valuable token (equal: lower slot; NaN counts as
+ * less than every number) among those whose position is at most length - recent, so that the newest `recent` tokens, the
+ * new one among them, stay; its slot_acc is its own summed weight, its rows are written in 4 bits.
+ *   weights: float[batch, n_heads, C + 1], entry C the new token's own.  k_new, v_new: T[batch, n_kv_heads, dh].
+ *   length: in and out, int32[batch, n_kv_heads]: position of the new token, advanced by one. Where it is negative, nothing
+ *           of that (sequence, head) is read or written but admit_slot and evicted_pos (both -1): a padded batch.
+ *   admit_slot, evicted_pos: out, int32[batch, n_kv_heads]; evicted_pos is -1 where an empty slot was taken.
+ * If no slot is empty and no position is old enough, the token is not admitted (both -1, ADORE_WORD_BOUNDS).
+ * Errors: INVALID_ARG, UNSUPPORTED, CUDA. */
+adore_status_t adore_evict_step(const adore_q4_t *cache, const float *weights, const void *k_new, const void *v_new,
+                                int32_t recent, void *cache_rows, int32_t *slot_pos, float *slot_acc, int32_t *length,
+                                int32_t *admit_slot, int32_t *evicted_pos, uint32_t *error_word, void *cuda_stream);
+
+/* Decode attention over the 4-bit rows of the occupied slots and the token's own full-precision row (Section 2.3's
+ * attention over the cached rows, without the top-K mask).
+ *   q, out: T[batch, n_heads, dh].  k_new, v_new: T[batch, n_kv_heads, dh], or both NULL: the cached rows alone.
+ *   weights: float[batch, n_heads, C + 1] or NULL; 0 for empty slots (and for entry C without k_new).
+ * A head with nothing to attend to gets zeros. Errors: INVALID_ARG, UNSUPPORTED, CUDA. */
+adore_status_t adore_q4_attention(const adore_q4_t *cache, const void *q, const void *k_new, const void *v_new,
+                                  const void *cache_rows, const int32_t *slot_pos, void *out, float *weights,
+                                  void *cuda_stream);
+
+/* The values that cache rows stand for: k_out, v_out T[batch, n_kv_heads, n, dh] of slots slots[b, g, i] (int32; outside
+ * [0, C): zeros), or of all slots in order when slots is NULL (n = C). For checking, and for moving rows back to a cache
+ * in full precision (Section 2.1's rows). Errors: INVALID_ARG, UNSUPPORTED, CUDA. */
+adore_status_t adore_q4_read(const adore_q4_t *cache, const void *cache_rows, const int32_t *slots, int32_t n,
+                             void *k_out, void *v_out, void *cuda_stream);
+
 const char *adore_status_string(adore_status_t s);
 
 #ifdef __cplusplus

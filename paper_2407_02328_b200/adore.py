@@ -46,6 +46,18 @@ class adore_controller_weights_t(C.Structure):
                                           "mlp_w1", "mlp_b1", "mlp_w2", "mlp_b2")]
 
 
+class adore_prompt_t(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("dtype", C.c_int), ("n_seqs", C.c_int32), ("total", C.c_int32),
+                ("n_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("scale", C.c_float),
+                ("q_row", C.c_int64), ("q_head", C.c_int64), ("k_row", C.c_int64), ("k_head", C.c_int64),
+                ("v_row", C.c_int64), ("v_head", C.c_int64), ("out_row", C.c_int64), ("out_head", C.c_int64)]
+
+
+class adore_q4_t(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("dtype", C.c_int), ("batch", C.c_int32), ("n_heads", C.c_int32),
+                ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("capacity", C.c_int32), ("scale", C.c_float)]
+
+
 _LIB = None
 EXPORTS = ["adore_cache_create", "adore_cache_destroy", "adore_cache_set_projection",
            "adore_cache_append_tokens", "adore_cache_fill_layer", "adore_decode_step",
@@ -55,7 +67,9 @@ EXPORTS = ["adore_cache_create", "adore_cache_destroy", "adore_cache_set_project
            "adore_cache_set_stage_timing", "adore_cache_stage_times", "adore_cache_group_times", "adore_cache_rebuild_rows",
            "adore_controller_score_static",
            "adore_cache_export_state", "adore_cache_import_state", "adore_step_begin", "adore_attend_rows",
-           "adore_label_tokens", "adore_decode_rebuild_host", "adore_decode_rebuild_host_queued", "adore_cache_wait_outputs"]
+           "adore_label_tokens", "adore_decode_rebuild_host", "adore_decode_rebuild_host_queued", "adore_cache_wait_outputs",
+           "adore_prompt_attention", "adore_prompt_weights", "adore_q4_bytes", "adore_evict_prompt", "adore_evict_step",
+           "adore_q4_attention", "adore_q4_read"]
 
 
 def _lib():
@@ -101,6 +115,15 @@ def _lib():
         lib.adore_cache_import_state.argtypes = [vp, vp, C.c_size_t]
         lib.adore_controller_score_static.argtypes = [C.POINTER(adore_controller_weights_t), C.c_int, i32, i32, i32, vp, vp,
                                                       i32, C.c_float, vp, vp, vp]
+        prompt, q4 = C.POINTER(adore_prompt_t), C.POINTER(adore_q4_t)
+        lib.adore_prompt_attention.argtypes = [prompt] + [vp] * 8
+        lib.adore_prompt_weights.argtypes = [prompt, vp, vp, vp, vp, i32, vp, vp, vp]
+        lib.adore_q4_bytes.argtypes = [q4]
+        lib.adore_q4_bytes.restype = C.c_size_t
+        lib.adore_evict_prompt.argtypes = [q4, prompt, vp, vp, vp, vp, i32] + [vp] * 6
+        lib.adore_evict_step.argtypes = [q4, vp, vp, vp, i32] + [vp] * 8
+        lib.adore_q4_attention.argtypes = [q4] + [vp] * 8
+        lib.adore_q4_read.argtypes = [q4, vp, vp, i32, vp, vp, vp]
         _LIB = lib
     return _LIB
 
@@ -286,6 +309,192 @@ def adore_controller_score_static(weights_dev: Dict[str, object], dtype: str, ba
     _check(_lib().adore_controller_score_static(C.byref(w), ADORE_F32 if dtype == "f32" else ADORE_BF16, batch, hidden,
                                                 ctrl_hidden, _ptr(x), _ptr(z), position, pos_scale, _ptr(score),
                                                 _ptr(sigma), cuda_stream or None), "adore_controller_score_static")
+
+
+# ---- whole prompts, eviction by attention weight, rows in 4 bits ---------------------------------
+# These calls take torch tensors and read shapes, strides and the element type from them. Tensors have to lie on the
+# current device; work is queued on torch's current stream unless a stream is given.
+def _refuse(where: str, why: str):
+    raise AdoreError(1, f"{where}: {why}")
+
+
+def _tensors(where: str, given) -> None:
+    """given: (name, tensor or None, dtype, shape or None). Contiguous CUDA tensors of the current device, or None."""
+    import torch
+    device = None
+    for name, t, dtype, shape in given:
+        if t is None:
+            continue
+        if t.dtype != dtype:
+            _refuse(where, f"{name} is {t.dtype}, not {dtype}")
+        if t.is_cuda and device is None:
+            device = torch.cuda.current_device()
+        if not t.is_cuda or t.get_device() != device:
+            _refuse(where, f"{name} is on {t.device}, not on the current device")
+        if shape is not None:
+            if t.shape != shape:
+                _refuse(where, f"{name} has shape {tuple(t.shape)}, not {tuple(shape)}")
+            if not t.is_contiguous():
+                _refuse(where, f"{name} is not contiguous")
+
+
+def _elem(where: str, t) -> int:
+    import torch
+    if t.dtype == torch.bfloat16:
+        return ADORE_BF16
+    if t.dtype == torch.float32:
+        return ADORE_F32
+    _refuse(where, f"element type {t.dtype}")
+
+
+def _stream(cuda_stream) -> Optional[int]:
+    if cuda_stream is None:
+        import torch
+        cuda_stream = torch.cuda.current_stream().cuda_stream
+    return cuda_stream or None
+
+
+def _at(t) -> Optional[int]:
+    return None if t is None else t.data_ptr()
+
+
+def _packed(where: str, seq_start, q, k, v, out, scale: float, n_heads: Optional[int] = None) -> adore_prompt_t:
+    """The shape of packed rows [total, heads, head_dim]; q, v and out may be missing."""
+    import torch
+    if k.dim() != 3 or seq_start.dim() != 1 or seq_start.numel() < 2:
+        _refuse(where, "k is [total, kv_heads, head_dim], seq_start int32 [sequences + 1]")
+    total, hk, dh = k.shape
+    if q is not None:
+        if q.dim() != 3:
+            _refuse(where, "q is [total, heads, head_dim]")
+        n_heads = q.shape[1]
+    p = adore_prompt_t(struct_size=C.sizeof(adore_prompt_t), dtype=_elem(where, k), n_seqs=seq_start.numel() - 1, total=total,
+                       n_heads=n_heads, n_kv_heads=hk, head_dim=dh, scale=scale)
+    for name, t, heads in (("q", q, n_heads), ("k", k, hk), ("v", v, hk), ("out", out, n_heads)):
+        if t is None:
+            continue
+        if t.shape != (total, heads, dh):
+            _refuse(where, f"{name} has shape {tuple(t.shape)}, not {(total, heads, dh)}")
+        if t.stride(2) != 1:
+            _refuse(where, f"the elements of a row of {name} are not consecutive")
+        setattr(p, name + "_row", t.stride(0))
+        setattr(p, name + "_head", t.stride(1))
+    _tensors(where, [("seq_start", seq_start, torch.int32, seq_start.shape)] +
+             [(name, t, k.dtype, None) for name, t in (("q", q), ("k", k), ("v", v), ("out", out))])
+    return p
+
+
+def adore_prompt_attention(q, k, v, seq_start, out, lse=None, scale: float = 0.0, error_word=None, cuda_stream=None) -> None:
+    """Causal attention of packed prompts: q, out [total, heads, dh], k, v [total, kv_heads, dh] (strided rows are fine),
+    seq_start int32 [sequences + 1], lse float32 [heads, total] or None, error_word int32 [1] or None."""
+    import torch
+    where = "adore_prompt_attention"
+    p = _packed(where, seq_start, q, k, v, out, scale)
+    _tensors(where, (("lse", lse, torch.float32, (p.n_heads, p.total)), ("error_word", error_word, torch.int32, (1,))))
+    _check(_lib().adore_prompt_attention(C.byref(p), _at(seq_start), _at(q), _at(k), _at(v), _at(out), _at(lse), _at(error_word),
+                                         _stream(cuda_stream)), where)
+
+
+def adore_prompt_weights(q, k, lse, seq_start, acc, window: int = 0, scale: float = 0.0, error_word=None, cuda_stream=None) -> None:
+    """Attention weight every prompt token received: acc float32 [kv_heads, total]; window: only the last queries count."""
+    import torch
+    where = "adore_prompt_weights"
+    p = _packed(where, seq_start, q, k, None, None, scale)
+    _tensors(where, (("lse", lse, torch.float32, (p.n_heads, p.total)), ("acc", acc, torch.float32, (p.n_kv_heads, p.total)),
+                     ("error_word", error_word, torch.int32, (1,))))
+    _check(_lib().adore_prompt_weights(C.byref(p), _at(seq_start), _at(q), _at(k), _at(lse), window, _at(acc), _at(error_word),
+                                       _stream(cuda_stream)), where)
+
+
+def _q4(where: str, like, batch: int, n_heads: int, n_kv_heads: int, head_dim: int, capacity: int, cache, scale: float = 0.0) -> adore_q4_t:
+    import torch
+    c = adore_q4_t(struct_size=C.sizeof(adore_q4_t), dtype=_elem(where, like), batch=batch, n_heads=n_heads, n_kv_heads=n_kv_heads,
+                   head_dim=head_dim, capacity=capacity, scale=scale)
+    _tensors(where, (("cache", cache, torch.uint8, cache.shape),))
+    need = _lib().adore_q4_bytes(C.byref(c))
+    if need and cache.numel() < need:
+        _refuse(where, f"the cache has {cache.numel()} bytes, {need} are needed")
+    return c
+
+
+def adore_q4_bytes(batch: int, n_kv_heads: int, head_dim: int, capacity: int) -> int:
+    """Bytes of a 4-bit cache buffer (a uint8 tensor)."""
+    c = adore_q4_t(struct_size=C.sizeof(adore_q4_t), dtype=ADORE_BF16, batch=batch, n_heads=n_kv_heads, n_kv_heads=n_kv_heads,
+                   head_dim=head_dim, capacity=capacity, scale=0.0)
+    n = _lib().adore_q4_bytes(C.byref(c))
+    if n == 0:
+        _refuse("adore_q4_bytes", "shape not supported")
+    return n
+
+
+def adore_evict_prompt(acc, k, v, seq_start, recent: int, cache, slot_pos, slot_acc, length, error_word=None, cuda_stream=None) -> None:
+    """Fills a 4-bit cache from packed prompts: slot_pos int32 and slot_acc float32 [sequences, kv_heads, capacity], length
+    int32 [sequences, kv_heads], acc float32 [kv_heads, total] as adore_prompt_weights wrote it."""
+    import torch
+    where = "adore_evict_prompt"
+    p = _packed(where, seq_start, None, k, v, None, 0.0, n_heads=k.shape[1] if k.dim() == 3 else 0)
+    if slot_pos.dim() != 3:
+        _refuse(where, "slot_pos is int32 [sequences, kv_heads, capacity]")
+    shape = (p.n_seqs, p.n_kv_heads, slot_pos.shape[2])
+    c = _q4(where, k, p.n_seqs, p.n_heads, p.n_kv_heads, p.head_dim, shape[2], cache)
+    _tensors(where, (("acc", acc, torch.float32, (p.n_kv_heads, p.total)), ("slot_pos", slot_pos, torch.int32, shape),
+                     ("slot_acc", slot_acc, torch.float32, shape), ("length", length, torch.int32, shape[:2]),
+                     ("error_word", error_word, torch.int32, (1,))))
+    _check(_lib().adore_evict_prompt(C.byref(c), C.byref(p), _at(seq_start), _at(acc), _at(k), _at(v), recent, _at(cache), _at(slot_pos),
+                                     _at(slot_acc), _at(length), _at(error_word), _stream(cuda_stream)), where)
+
+
+def adore_evict_step(weights, k_new, v_new, recent: int, cache, slot_pos, slot_acc, length, admit_slot, evicted_pos, error_word=None,
+                     cuda_stream=None) -> None:
+    """One step's eviction: weights float32 [batch, heads, capacity + 1], k_new, v_new [batch, kv_heads, dh], the state of
+    adore_evict_prompt, admit_slot and evicted_pos int32 [batch, kv_heads]."""
+    import torch
+    where = "adore_evict_step"
+    if weights.dim() != 3 or k_new.dim() != 3 or slot_pos.dim() != 3:
+        _refuse(where, "weights [batch, heads, capacity + 1], k_new [batch, kv_heads, dh], slot_pos [batch, kv_heads, capacity]")
+    b, hk, dh = k_new.shape
+    h, cap = weights.shape[1], slot_pos.shape[2]
+    c = _q4(where, k_new, b, h, hk, dh, cap, cache)
+    _tensors(where, (("weights", weights, torch.float32, (b, h, cap + 1)), ("k_new", k_new, k_new.dtype, (b, hk, dh)),
+                     ("v_new", v_new, k_new.dtype, (b, hk, dh)), ("slot_pos", slot_pos, torch.int32, (b, hk, cap)),
+                     ("slot_acc", slot_acc, torch.float32, (b, hk, cap)), ("length", length, torch.int32, (b, hk)),
+                     ("admit_slot", admit_slot, torch.int32, (b, hk)), ("evicted_pos", evicted_pos, torch.int32, (b, hk)),
+                     ("error_word", error_word, torch.int32, (1,))))
+    _check(_lib().adore_evict_step(C.byref(c), _at(weights), _at(k_new), _at(v_new), recent, _at(cache), _at(slot_pos), _at(slot_acc),
+                                   _at(length), _at(admit_slot), _at(evicted_pos), _at(error_word), _stream(cuda_stream)), where)
+
+
+def adore_q4_attention(q, k_new, v_new, cache, slot_pos, out, weights=None, scale: float = 0.0, cuda_stream=None) -> None:
+    """Decode attention over 4-bit rows: q, out [batch, heads, dh], k_new, v_new [batch, kv_heads, dh] or both None, slot_pos
+    int32 [batch, kv_heads, capacity], weights float32 [batch, heads, capacity + 1] or None."""
+    import torch
+    where = "adore_q4_attention"
+    if q.dim() != 3 or slot_pos.dim() != 3:
+        _refuse(where, "q [batch, heads, dh], slot_pos [batch, kv_heads, capacity]")
+    b, h, dh = q.shape
+    hk, cap = slot_pos.shape[1:]
+    c = _q4(where, q, b, h, hk, dh, cap, cache, scale)
+    _tensors(where, (("q", q, q.dtype, (b, h, dh)), ("k_new", k_new, q.dtype, (b, hk, dh)), ("v_new", v_new, q.dtype, (b, hk, dh)),
+                     ("slot_pos", slot_pos, torch.int32, (b, hk, cap)), ("out", out, q.dtype, (b, h, dh)),
+                     ("weights", weights, torch.float32, (b, h, cap + 1))))
+    _check(_lib().adore_q4_attention(C.byref(c), _at(q), _at(k_new), _at(v_new), _at(cache), _at(slot_pos), _at(out), _at(weights),
+                                     _stream(cuda_stream)), where)
+
+
+def adore_q4_read(cache, capacity: int, slots, k_out, v_out, cuda_stream=None) -> None:
+    """The values of cache rows: k_out, v_out [batch, kv_heads, n, dh] of the slots int32 [batch, kv_heads, n] (or, for n = 1,
+    [batch, kv_heads]); slots None: all of them in order."""
+    import torch
+    where = "adore_q4_read"
+    if k_out.dim() != 4:
+        _refuse(where, "k_out [batch, kv_heads, n, dh]")
+    b, hk, n, dh = k_out.shape
+    c = _q4(where, k_out, b, hk, hk, dh, capacity, cache)
+    if slots is not None and slots.dim() == 2 and n == 1:
+        slots = slots.unsqueeze(2)
+    _tensors(where, (("slots", slots, torch.int32, (b, hk, n)), ("k_out", k_out, k_out.dtype, k_out.shape),
+                     ("v_out", v_out, k_out.dtype, k_out.shape)))
+    _check(_lib().adore_q4_read(C.byref(c), _at(cache), _at(slots), n, _at(k_out), _at(v_out), _stream(cuda_stream)), where)
 
 
 def adore_status_string(status: int) -> str:

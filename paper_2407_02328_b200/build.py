@@ -8,7 +8,7 @@ import sys
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB = os.path.join(HERE, "libadore.so")
-SOURCES = [os.path.join(HERE, "csrc", "adore_api.cu"), os.path.join(HERE, "csrc", "controller_static.cu")]
+SOURCES = [os.path.join(HERE, "csrc", n) for n in ("adore_api.cu", "controller_static.cu", "prompt_api.cu")]
 
 
 def _newest_source_mtime() -> float:

@@ -1,0 +1,91 @@
+// Packed sequences: how a CTA of a launch over all sequences finds the tile it works on.
+#pragma once
+
+#include "common.cuh"
+
+namespace adore {
+
+// Tensors of packed rows; strides in elements.
+struct PackedParams {
+  const int* seq_start;       // [S + 1] device
+  int S, total;
+  int H, Hk, group;           // query heads, key/value heads, query heads per key/value head
+  float scale;
+  long long q_row, q_head, k_row, k_head, v_row, v_head, out_row, out_head;
+  unsigned* err;              // or nullptr
+};
+
+struct PackedTile {
+  int seq, start, len;        // the sequence, its first packed row, its rows
+  int index;                  // tile within the sequence
+};
+
+// Rows of sequence s, or 0 (and the bounds bit) if its ends do not fit the packed tensors.
+__device__ __forceinline__ int packed_len(const int* seq_start, int s, int total, unsigned* err) {
+  const int a = __ldg(seq_start + s), b = __ldg(seq_start + s + 1);
+  if (a < 0 || b < a || b > total) {
+    if (err != nullptr) set_error(err, ERRW_BOUNDS);
+    return 0;
+  }
+  return b - a;
+}
+
+// The tile of BLOCK rows with the given rank, tiles counted from the highest index within their sequence down (all last
+// tiles of the longest sequences first). Under a causal mask the work of a tile grows with its index, so a launch whose
+// CTAs take their rank from blockIdx starts the longest ones first and ends evenly. One warp calls it; no table and no
+// workspace is needed: the number of tiles with an index >= p is a sum over the sequences, p is found by bisection.
+// Returns false if there are fewer tiles.
+template <int BLOCK>
+__device__ __forceinline__ bool find_packed_tile(const int* seq_start, int S, int total, int rank, unsigned* err, PackedTile& t) {
+  const int lane = threadIdx.x & 31;
+  int top = 0, all = 0;
+  for (int s = lane; s < S; s += 32) {
+    const int n = (packed_len(seq_start, s, total, err) + BLOCK - 1) / BLOCK;
+    top = max(top, n);
+    all += n;
+  }
+  all = warp_sum(all);
+  top = __reduce_max_sync(0xffffffffu, top);
+  if (rank >= all) return false;
+  int lo = 0, hi = top, above = 0;           // tiles with index >= lo: more than rank; with index >= hi: `above` <= rank
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    int n = 0;
+    for (int s = lane; s < S; s += 32) n += max(0, (packed_len(seq_start, s, total, nullptr) + BLOCK - 1) / BLOCK - mid);
+    n = warp_sum(n);
+    if (n > rank) lo = mid;
+    else { hi = mid; above = n; }
+  }
+  int want = rank - above;                   // the want-th sequence with more than lo tiles
+  for (int s0 = 0; s0 < S; s0 += 32) {
+    const int s = s0 + lane;
+    const int len = s < S ? packed_len(seq_start, s, total, nullptr) : 0;
+    const unsigned has = __ballot_sync(0xffffffffu, (len + BLOCK - 1) / BLOCK > lo);
+    const int n = __popc(has);
+    if (want < n) {
+      const int src = __fns(has, 0, want + 1);
+      t.seq = s0 + src;
+      t.len = __shfl_sync(0xffffffffu, len, src);
+      t.start = __ldg(seq_start + t.seq);
+      t.index = lo;
+      return true;
+    }
+    want -= n;
+  }
+  return false;
+}
+
+// Four consecutive elements as floats.
+__device__ __forceinline__ float4 load4(const float* p) { return *reinterpret_cast<const float4*>(p); }
+__device__ __forceinline__ float4 load4(const __nv_bfloat16* p) {
+  const uint2 r = *reinterpret_cast<const uint2*>(p);
+  return make_float4(__uint_as_float(r.x << 16), __uint_as_float(r.x & 0xffff0000u), __uint_as_float(r.y << 16),
+                     __uint_as_float(r.y & 0xffff0000u));
+}
+__device__ __forceinline__ void store4(float* p, float4 v) { *reinterpret_cast<float4*>(p) = v; }
+__device__ __forceinline__ void store4(__nv_bfloat16* p, float4 v) {
+  const __nv_bfloat162 a = __floats2bfloat162_rn(v.x, v.y), b = __floats2bfloat162_rn(v.z, v.w);
+  *reinterpret_cast<uint2*>(p) = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
+}
+
+}  // namespace adore

@@ -1,0 +1,264 @@
+// Host side of the calls for whole prompts, eviction by attention weight and the 4-bit cache: argument checks and launches.
+#include <algorithm>
+#include <cmath>
+#include <initializer_list>
+
+#include "../../include/adore.h"
+#include "evict.cuh"
+#include "prompt_attention.cuh"
+#include "q4_attention.cuh"
+
+using namespace adore;
+
+namespace {
+
+bool aligned16(std::initializer_list<const void*> ps) {
+  for (const void* p : ps)
+    if (reinterpret_cast<uintptr_t>(p) & 15u) return false;
+  return true;
+}
+bool aligned4(std::initializer_list<const void*> ps) {
+  for (const void* p : ps)
+    if (reinterpret_cast<uintptr_t>(p) & 3u) return false;
+  return true;
+}
+
+constexpr int64_t kMaxStride = int64_t(1) << 38;      // elements; bytes stay below the 2^40 of a tensor map
+constexpr int64_t kMaxGrid = 2147483647;
+
+// Strides of one packed tensor: whole 16-byte pieces; a dimension of one element may have any stride.
+bool check_strides(int64_t& row, int64_t& head, int64_t rows, int64_t heads, int dh, int per16, bool written) {
+  if (rows <= 1) row = std::max<int64_t>(dh, heads > 1 ? std::min(std::max<int64_t>(head, 0), kMaxStride) : 0);
+  if (heads <= 1) head = dh;
+  if (row < 0 || head < 0 || row > kMaxStride || head > kMaxStride || row % per16 != 0 || head % per16 != 0) return false;
+  if (row < dh || head < dh) return false;
+  // the last element's offset has to fit 63 bits with its bytes
+  if (row * (rows > 0 ? rows - 1 : 0) > (int64_t(1) << 58) || head * (heads - 1) > (int64_t(1) << 58)) return false;
+  if (written && rows > 1 && heads > 1) {
+    const bool rows_inner = row < head;
+    if (rows_inner ? head < row * (rows - 1) + dh : row < head * (heads - 1) + dh) return false;
+  }
+  return true;
+}
+
+adore_status_t check_heads(int n_heads, int n_kv_heads, int head_dim, adore_dtype_t dtype, float scale) {
+  if (n_heads < 1 || n_kv_heads < 1 || head_dim < 1 || n_heads % n_kv_heads != 0) return ADORE_ERR_INVALID_ARG;
+  if (dtype != ADORE_F32 && dtype != ADORE_BF16) return ADORE_ERR_INVALID_ARG;
+  if (!std::isfinite(scale)) return ADORE_ERR_INVALID_ARG;
+  if (head_dim != 64 && head_dim != 128) return ADORE_ERR_UNSUPPORTED;
+  return ADORE_OK;
+}
+float scale_of(float scale, int head_dim) { return scale != 0.f ? scale : 1.f / std::sqrt(float(head_dim)); }
+
+// Checks a packed shape and fills the kernels' parameters; `with_q`, `with_v`, `with_out`: which strides count.
+adore_status_t packed_params(const adore_prompt_t* s, const int32_t* seq_start, uint32_t* err, bool with_q, bool with_v, bool with_out,
+                             PackedParams& p) {
+  if (!s || s->struct_size != sizeof(adore_prompt_t) || !seq_start || s->n_seqs < 1 || s->total < 0) return ADORE_ERR_INVALID_ARG;
+  const adore_status_t st = check_heads(s->n_heads, s->n_kv_heads, s->head_dim, s->dtype, s->scale);
+  if (st != ADORE_OK) return st;
+  if (!aligned4({seq_start, err})) return ADORE_ERR_INVALID_ARG;
+  p.seq_start = seq_start; p.S = s->n_seqs; p.total = s->total;
+  p.H = s->n_heads; p.Hk = s->n_kv_heads; p.group = s->n_heads / s->n_kv_heads;
+  p.scale = scale_of(s->scale, s->head_dim);
+  p.q_row = s->q_row; p.q_head = s->q_head; p.k_row = s->k_row; p.k_head = s->k_head;
+  p.v_row = s->v_row; p.v_head = s->v_head; p.out_row = s->out_row; p.out_head = s->out_head;
+  p.err = err;
+  const int per16 = s->dtype == ADORE_F32 ? 4 : 8;
+  int64_t strides[8] = {p.q_row, p.q_head, p.k_row, p.k_head, p.v_row, p.v_head, p.out_row, p.out_head};
+  if ((with_q && !check_strides(strides[0], strides[1], s->total, s->n_heads, s->head_dim, per16, false)) ||
+      !check_strides(strides[2], strides[3], s->total, s->n_kv_heads, s->head_dim, per16, false) ||
+      (with_v && !check_strides(strides[4], strides[5], s->total, s->n_kv_heads, s->head_dim, per16, false)) ||
+      (with_out && !check_strides(strides[6], strides[7], s->total, s->n_heads, s->head_dim, per16, true)))
+    return ADORE_ERR_INVALID_ARG;
+  p.q_row = strides[0]; p.q_head = strides[1]; p.k_row = strides[2]; p.k_head = strides[3];
+  p.v_row = strides[4]; p.v_head = strides[5]; p.out_row = strides[6]; p.out_head = strides[7];
+  return ADORE_OK;
+}
+
+// CTAs of a launch over all tiles of `block` rows and `heads` heads; 0 if they do not fit a grid.
+unsigned tile_grid(const PackedParams& p, int block, int heads) {
+  const int64_t n = (int64_t(p.total) / block + p.S) * heads;
+  return n <= kMaxGrid ? unsigned(n) : 0u;
+}
+
+adore_status_t launched() { return cudaGetLastError() == cudaSuccess ? ADORE_OK : ADORE_ERR_CUDA; }
+
+template <typename K>
+bool allow_smem(K kernel, size_t bytes) {
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(bytes)) == cudaSuccess) return true;
+  cudaGetLastError();
+  return false;
+}
+
+template <typename T, int DH>
+adore_status_t attention_simt(const PackedParams& p, const void* q, const void* k, const void* v, void* out, float* lse, cudaStream_t st) {
+  const unsigned grid = tile_grid(p, kPsBlock, p.H);
+  if (grid == 0) return ADORE_ERR_UNSUPPORTED;
+  if (!allow_smem(prompt_attention_simt_kernel<T, DH>, prompt_simt_smem<DH>())) return ADORE_ERR_CUDA;
+  prompt_attention_simt_kernel<T, DH><<<grid, kPsThreads, prompt_simt_smem<DH>(), st>>>(
+      p, static_cast<const T*>(q), static_cast<const T*>(k), static_cast<const T*>(v), static_cast<T*>(out), lse);
+  return launched();
+}
+
+template <typename T, int DH>
+adore_status_t weights_simt(const PackedParams& p, const void* q, const void* k, const float* lse, int window, float* acc, cudaStream_t st) {
+  const unsigned grid = tile_grid(p, kPsBlock, p.Hk);
+  if (grid == 0) return ADORE_ERR_UNSUPPORTED;
+  if (!allow_smem(prompt_weights_simt_kernel<T, DH>, prompt_weights_simt_smem<DH>())) return ADORE_ERR_CUDA;
+  prompt_weights_simt_kernel<T, DH><<<grid, kPsThreads, prompt_weights_simt_smem<DH>(), st>>>(
+      p, static_cast<const T*>(q), static_cast<const T*>(k), lse, window, acc);
+  return launched();
+}
+
+adore_status_t check_q4(const adore_q4_t* c) {
+  if (!c || c->struct_size != sizeof(adore_q4_t) || c->batch < 1 || c->capacity < 1) return ADORE_ERR_INVALID_ARG;
+  const adore_status_t st = check_heads(c->n_heads, c->n_kv_heads, c->head_dim, c->dtype, c->scale);
+  if (st != ADORE_OK) return st;
+  // slot indices take 31 bits of a key, and every (sequence, head) is a CTA
+  if (c->capacity > (1 << 30) || int64_t(c->batch) * c->n_heads > kMaxGrid) return ADORE_ERR_UNSUPPORTED;
+  return ADORE_OK;
+}
+size_t q4_row_count(const adore_q4_t* c) { return size_t(c->batch) * c->n_kv_heads; }
+
+template <typename T, int DH>
+adore_status_t pack_rows(const adore_q4_t* c, const PackedParams& p, const void* k, const void* v, const int* slot_pos, const int* length,
+                         const Q4Rows& rows, cudaStream_t st) {
+  constexpr int kRows = 256 / (DH / 8);
+  const int P = q4_padded(c->capacity);
+  const size_t R = q4_row_count(c);
+  if (R > 65535) return ADORE_ERR_UNSUPPORTED;
+  const dim3 grid(unsigned((P + kRows - 1) / kRows), unsigned(R));
+  evict_pack_kernel<T, DH><<<grid, 256, 0, st>>>(p, static_cast<const T*>(k), static_cast<const T*>(v), slot_pos, length, c->capacity, P, rows);
+  return launched();
+}
+
+template <typename T, int DH>
+adore_status_t step_rows(const adore_q4_t* c, const float* weights, const void* k, const void* v, int recent, const Q4Rows& rows,
+                         int* slot_pos, float* slot_acc, int* length, int* admit, int* evicted, unsigned* err, cudaStream_t st) {
+  evict_step_kernel<T, DH><<<unsigned(q4_row_count(c)), 256, 0, st>>>(weights, static_cast<const T*>(k), static_cast<const T*>(v), c->n_heads,
+                                                                      c->n_kv_heads, c->capacity, q4_padded(c->capacity), recent, rows,
+                                                                      slot_pos, slot_acc, length, admit, evicted, err);
+  return launched();
+}
+
+template <typename T, int DH>
+adore_status_t attend_q4(const adore_q4_t* c, const void* q, const void* k, const void* v, const Q4Rows& rows, const int* slot_pos, void* out,
+                         float* weights, cudaStream_t st) {
+  q4_attention_simple_kernel<T, DH><<<unsigned(c->batch * c->n_heads), 32, 0, st>>>(
+      rows, c->n_heads, c->n_kv_heads, c->capacity, q4_padded(c->capacity), scale_of(c->scale, DH), static_cast<const T*>(q),
+      static_cast<const T*>(k), static_cast<const T*>(v), slot_pos, static_cast<T*>(out), weights);
+  return launched();
+}
+
+template <typename T, int DH>
+adore_status_t read_rows(const adore_q4_t* c, const Q4Rows& rows, const int* slots, int n, void* k, void* v, cudaStream_t st) {
+  const size_t pieces = q4_row_count(c) * n * (DH / 8);
+  const unsigned grid = unsigned(std::min<size_t>((pieces + 255) / 256, 148 * 64));
+  q4_read_kernel<T, DH><<<grid, 256, 0, st>>>(rows, q4_padded(c->capacity), c->capacity, slots, n, pieces, static_cast<T*>(k),
+                                              static_cast<T*>(v));
+  return launched();
+}
+
+// The four instances of a call, by element type and head dimension.
+#define ADORE_BY_TYPE(dtype, dh, fn, ...)                                                                        \
+  ((dtype) == ADORE_F32 ? ((dh) == 64 ? fn<float, 64>(__VA_ARGS__) : fn<float, 128>(__VA_ARGS__))               \
+                        : ((dh) == 64 ? fn<__nv_bfloat16, 64>(__VA_ARGS__) : fn<__nv_bfloat16, 128>(__VA_ARGS__)))
+
+}  // namespace
+
+extern "C" {
+
+adore_status_t adore_prompt_attention(const adore_prompt_t* shape, const int32_t* seq_start, const void* q, const void* k,
+                                      const void* v, void* out, float* lse, uint32_t* error_word, void* cuda_stream) {
+  PackedParams p{};
+  const adore_status_t s = packed_params(shape, seq_start, error_word, true, true, true, p);
+  if (s != ADORE_OK) return s;
+  if (shape->total == 0) return ADORE_OK;
+  if (!q || !k || !v || !out || !aligned16({q, k, v, out}) || !aligned4({lse})) return ADORE_ERR_INVALID_ARG;
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  return ADORE_BY_TYPE(shape->dtype, shape->head_dim, attention_simt, p, q, k, v, out, lse, st);
+}
+
+adore_status_t adore_prompt_weights(const adore_prompt_t* shape, const int32_t* seq_start, const void* q, const void* k,
+                                    const float* lse, int32_t window, float* acc, uint32_t* error_word, void* cuda_stream) {
+  PackedParams p{};
+  const adore_status_t s = packed_params(shape, seq_start, error_word, true, false, false, p);
+  if (s != ADORE_OK) return s;
+  if (window < 0) return ADORE_ERR_INVALID_ARG;
+  if (shape->total == 0) return ADORE_OK;
+  if (!q || !k || !lse || !acc || !aligned16({q, k}) || !aligned4({lse, acc})) return ADORE_ERR_INVALID_ARG;
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  return ADORE_BY_TYPE(shape->dtype, shape->head_dim, weights_simt, p, q, k, lse, window, acc, st);
+}
+
+size_t adore_q4_bytes(const adore_q4_t* shape) {
+  if (check_q4(shape) != ADORE_OK) return 0;
+  const size_t R = q4_row_count(shape);
+  const int P = q4_padded(shape->capacity);
+  return 2 * (q4_code_bytes(R, P, shape->head_dim) + q4_pair_bytes(R, P, shape->head_dim));
+}
+
+adore_status_t adore_evict_prompt(const adore_q4_t* cache, const adore_prompt_t* rows, const int32_t* seq_start, const float* acc,
+                                  const void* k, const void* v, int32_t recent, void* cache_rows, int32_t* slot_pos, float* slot_acc,
+                                  int32_t* length, uint32_t* error_word, void* cuda_stream) {
+  adore_status_t s = check_q4(cache);
+  if (s != ADORE_OK) return s;
+  PackedParams p{};
+  s = packed_params(rows, seq_start, error_word, false, true, false, p);
+  if (s != ADORE_OK) return s;
+  if (rows->n_seqs != cache->batch || rows->n_heads != cache->n_heads || rows->n_kv_heads != cache->n_kv_heads ||
+      rows->head_dim != cache->head_dim || rows->dtype != cache->dtype || recent < 1 || recent > cache->capacity)
+    return ADORE_ERR_INVALID_ARG;
+  if (!cache_rows || !slot_pos || !slot_acc || !length || !aligned16({cache_rows}) || !aligned4({slot_pos, slot_acc, length}))
+    return ADORE_ERR_INVALID_ARG;
+  if (rows->total > 0 && (!acc || !k || !v || !aligned16({k, v}) || !aligned4({acc}))) return ADORE_ERR_INVALID_ARG;
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  evict_select_kernel<<<unsigned(q4_row_count(cache)), kEvictThreads, 0, st>>>(seq_start, rows->total, cache->n_kv_heads, cache->capacity,
+                                                                               recent, acc, slot_pos, slot_acc, length, error_word);
+  s = launched();
+  if (s != ADORE_OK) return s;
+  const Q4Rows c = q4_rows(cache_rows, q4_row_count(cache), q4_padded(cache->capacity), cache->head_dim);
+  return ADORE_BY_TYPE(cache->dtype, cache->head_dim, pack_rows, cache, p, k, v, slot_pos, length, c, st);
+}
+
+adore_status_t adore_evict_step(const adore_q4_t* cache, const float* weights, const void* k_new, const void* v_new, int32_t recent,
+                                void* cache_rows, int32_t* slot_pos, float* slot_acc, int32_t* length, int32_t* admit_slot,
+                                int32_t* evicted_pos, uint32_t* error_word, void* cuda_stream) {
+  const adore_status_t s = check_q4(cache);
+  if (s != ADORE_OK) return s;
+  if (recent < 1 || recent > cache->capacity || !weights || !k_new || !v_new || !cache_rows || !slot_pos || !slot_acc || !length ||
+      !admit_slot || !evicted_pos || !aligned16({k_new, v_new, cache_rows}) ||
+      !aligned4({weights, slot_pos, slot_acc, length, admit_slot, evicted_pos, error_word}))
+    return ADORE_ERR_INVALID_ARG;
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  const Q4Rows c = q4_rows(cache_rows, q4_row_count(cache), q4_padded(cache->capacity), cache->head_dim);
+  return ADORE_BY_TYPE(cache->dtype, cache->head_dim, step_rows, cache, weights, k_new, v_new, recent, c, slot_pos, slot_acc, length,
+                       admit_slot, evicted_pos, error_word, st);
+}
+
+adore_status_t adore_q4_attention(const adore_q4_t* cache, const void* q, const void* k_new, const void* v_new, const void* cache_rows,
+                                  const int32_t* slot_pos, void* out, float* weights, void* cuda_stream) {
+  const adore_status_t s = check_q4(cache);
+  if (s != ADORE_OK) return s;
+  if (!q || !cache_rows || !slot_pos || !out || (k_new == nullptr) != (v_new == nullptr) ||
+      !aligned16({q, k_new, v_new, cache_rows, out}) || !aligned4({slot_pos, weights}))
+    return ADORE_ERR_INVALID_ARG;
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  const Q4Rows c = q4_rows(const_cast<void*>(cache_rows), q4_row_count(cache), q4_padded(cache->capacity), cache->head_dim);
+  return ADORE_BY_TYPE(cache->dtype, cache->head_dim, attend_q4, cache, q, k_new, v_new, c, slot_pos, out, weights, st);
+}
+
+adore_status_t adore_q4_read(const adore_q4_t* cache, const void* cache_rows, const int32_t* slots, int32_t n, void* k_out, void* v_out,
+                             void* cuda_stream) {
+  const adore_status_t s = check_q4(cache);
+  if (s != ADORE_OK) return s;
+  if (n < 0 || (slots == nullptr && n != cache->capacity) || !cache_rows || !aligned16({cache_rows, k_out, v_out}) || !aligned4({slots}))
+    return ADORE_ERR_INVALID_ARG;
+  if (n == 0) return ADORE_OK;
+  if (!k_out || !v_out) return ADORE_ERR_INVALID_ARG;
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  const Q4Rows c = q4_rows(const_cast<void*>(cache_rows), q4_row_count(cache), q4_padded(cache->capacity), cache->head_dim);
+  return ADORE_BY_TYPE(cache->dtype, cache->head_dim, read_rows, cache, c, slots, n, k_out, v_out, st);
+}
+
+}  // extern "C"

@@ -1,0 +1,135 @@
+// The 4-bit row format: groups of 64 elements with a bfloat16 step and low value, where codes lie, and reading rows back.
+//
+// The places of the codes serve the matrix instructions of the decode attention (m16n8k16, whose operands hold pairs of
+// neighbouring k): a lane that works on elements 8 t .. of every 32 of a key row finds them in one piece, and two
+// neighbouring slots share a word of the value part with their codes of the same elements 16 bits apart, which
+// is a pair of neighbouring k when the product runs over the slots. Codes of different slots never share 16 bits, so a row can
+// be written without reading its neighbour's.
+#pragma once
+
+#include "common.cuh"
+
+namespace adore {
+
+constexpr int kQ4Group = 64;
+constexpr int kQ4SlotPad = 16;
+
+__host__ __device__ inline int q4_padded(int capacity) { return (capacity + kQ4SlotPad - 1) / kQ4SlotPad * kQ4SlotPad; }
+
+// The parts of a cache buffer (see adore.h); R = batch * key/value heads.
+struct Q4Rows {
+  uint32_t* k;                // [R][P][4][dh/32]
+  uint32_t* v;                // [R][P/2][8][dh/32]
+  __nv_bfloat162* kp;         // [R][P][dh/64] step, low
+  __nv_bfloat162* vp;
+};
+__host__ __device__ inline size_t q4_code_bytes(size_t rows, int P, int dh) { return rows * P * (dh / 2); }
+__host__ __device__ inline size_t q4_pair_bytes(size_t rows, int P, int dh) { return rows * P * (dh / kQ4Group) * 4; }
+inline Q4Rows q4_rows(void* buf, size_t rows, int P, int dh) {
+  unsigned char* b = static_cast<unsigned char*>(buf);
+  const size_t codes = q4_code_bytes(rows, P, dh), pairs = q4_pair_bytes(rows, P, dh);
+  return Q4Rows{reinterpret_cast<uint32_t*>(b), reinterpret_cast<uint32_t*>(b + codes),
+                reinterpret_cast<__nv_bfloat162*>(b + 2 * codes), reinterpret_cast<__nv_bfloat162*>(b + 2 * codes + pairs)};
+}
+
+// Eight consecutive elements as floats.
+__device__ __forceinline__ void load8(const float* p, float (&x)[8]) {
+  const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
+  x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+}
+__device__ __forceinline__ void load8(const __nv_bfloat16* p, float (&x)[8]) {
+  Elem<__nv_bfloat16>::unpack(*reinterpret_cast<const uint4*>(p), x);
+}
+__device__ __forceinline__ void store8(float* p, const float (&x)[8]) {
+  *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
+  *reinterpret_cast<float4*>(p + 4) = make_float4(x[4], x[5], x[6], x[7]);
+}
+__device__ __forceinline__ void store8(__nv_bfloat16* p, const float (&x)[8]) {
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const __nv_bfloat162 t = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+    w[i] = *reinterpret_cast<const uint32_t*>(&t);
+  }
+  *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// Codes of 8 elements per lane; 8 neighbouring lanes hold a group. Every lane of the warp calls it. Low and step are rounded
+// to bfloat16 first and the codes chosen for the rounded values; the quotient is the correctly rounded one.
+__device__ __forceinline__ uint32_t q4_encode8(const float (&x)[8], __nv_bfloat162& pair) {
+  float lo = x[0], hi = x[0];
+#pragma unroll
+  for (int i = 1; i < 8; ++i) { lo = fminf(lo, x[i]); hi = fmaxf(hi, x[i]); }
+#pragma unroll
+  for (int o = 4; o > 0; o >>= 1) {
+    lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
+    hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
+  }
+  const __nv_bfloat16 low = __float2bfloat16_rn(lo);
+  const float lowf = __bfloat162float(low);
+  const __nv_bfloat16 step = __float2bfloat16_rn(__fdiv_rn(fmaxf(hi - lowf, 0.f), 15.f));
+  const float stepf = __bfloat162float(step);
+  pair = __halves2bfloat162(step, low);
+  uint32_t w = 0;
+  if (stepf > 0.f) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float t = fminf(fmaxf(rintf(__fdiv_rn(x[i] - lowf, stepf)), 0.f), 15.f);
+      w |= uint32_t(t) << (4 * i);
+    }
+  }
+  return w;
+}
+
+// Where elements 8 j .. 8 j + 7 of a key row stand: one word of the row's dh / 8.
+template <int DH>
+__device__ __forceinline__ int q4_k_word(int j) { return (DH / 32) * (j & 3) + (j >> 2); }
+// Where elements 8 j .. 8 j + 3 of a value row stand: a half of this word of the pair's dh / 4; 8 j + 4 .. in word + dh / 32.
+template <int DH>
+__device__ __forceinline__ int q4_v_word(int j) { return (DH / 32) * 2 * (j & 3) + (j >> 2); }
+
+// Writes one row of a slot: 8 elements' codes per lane (j = piece of the row), both of K and V.
+template <int DH>
+__device__ __forceinline__ void q4_store_piece(const Q4Rows& c, size_t r, int P, int slot, int j, uint32_t kw, __nv_bfloat162 kpair,
+                                               uint32_t vw, __nv_bfloat162 vpair) {
+  c.k[(r * P + slot) * (DH / 8) + q4_k_word<DH>(j)] = kw;
+  uint16_t* v = reinterpret_cast<uint16_t*>(c.v + (r * (P / 2) + slot / 2) * (DH / 4)) + (slot & 1);
+  v[2 * q4_v_word<DH>(j)] = uint16_t(vw & 0xffffu);
+  v[2 * (q4_v_word<DH>(j) + DH / 32)] = uint16_t(vw >> 16);
+  if ((j & 7) == 0) {
+    c.kp[(r * P + slot) * (DH / kQ4Group) + (j >> 3)] = kpair;
+    c.vp[(r * P + slot) * (DH / kQ4Group) + (j >> 3)] = vpair;
+  }
+}
+
+// Rows back to T: one thread per 8 elements of a listed row.
+template <typename T, int DH>
+__global__ void __launch_bounds__(256) q4_read_kernel(const Q4Rows c, int P, int C, const int* slots, int n, size_t pieces,
+                                                      T* k_out, T* v_out) {
+  for (size_t i = blockIdx.x * size_t(blockDim.x) + threadIdx.x; i < pieces; i += size_t(gridDim.x) * blockDim.x) {
+    const int j = int(i % (DH / 8));
+    const size_t row = i / (DH / 8), r = row / n;
+    const int slot = slots != nullptr ? slots[row] : int(row % n);
+    float kx[8], vx[8];
+    if (slot >= 0 && slot < C) {
+      const uint32_t kw = c.k[(r * P + slot) * (DH / 8) + q4_k_word<DH>(j)];
+      const uint32_t* vp = c.v + (r * (P / 2) + slot / 2) * (DH / 4) + q4_v_word<DH>(j);
+      const int sh = (slot & 1) * 16;
+      const uint32_t vw = ((vp[0] >> sh) & 0xffffu) | ((vp[DH / 32] >> sh) << 16);
+      const float2 ks = __bfloat1622float2(c.kp[(r * P + slot) * (DH / kQ4Group) + (j >> 3)]);
+      const float2 vs = __bfloat1622float2(c.vp[(r * P + slot) * (DH / kQ4Group) + (j >> 3)]);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        kx[e] = fmaf(float((kw >> (4 * e)) & 15u), ks.x, ks.y);      // the product is exact: 8 bits x 4 bits
+        vx[e] = fmaf(float((vw >> (4 * e)) & 15u), vs.x, vs.y);
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) kx[e] = vx[e] = 0.f;
+    }
+    store8(k_out + row * DH + 8 * j, kx);
+    store8(v_out + row * DH + 8 * j, vx);
+  }
+}
+
+}  // namespace adore

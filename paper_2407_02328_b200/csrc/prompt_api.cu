@@ -6,6 +6,7 @@
 #include "../../include/adore.h"
 #include "evict.cuh"
 #include "prompt_attention.cuh"
+#include "prompt_attention_tc.cuh"
 #include "q4_attention.cuh"
 
 using namespace adore;
@@ -110,6 +111,46 @@ adore_status_t weights_simt(const PackedParams& p, const void* q, const void* k,
   return launched();
 }
 
+// ---- tensor-core variants (bfloat16) --------------------------------------------------------------
+typedef CUresult (*EncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                             const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeFn tensor_map_encoder() {
+  static const EncodeFn fn = [] {
+    void* f = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &f, cudaEnableDefault, &q) != cudaSuccess || q != cudaDriverEntryPointSuccess) {
+      cudaGetLastError();
+      f = nullptr;
+    }
+    return reinterpret_cast<EncodeFn>(f);
+  }();
+  return fn;
+}
+
+// Packed rows as [row][head][element]: boxes of 128 rows x 64 elements of one head, 128-byte swizzle.
+bool packed_map(CUtensorMap* map, const void* base, int64_t row, int64_t head, int rows, int heads, int dh) {
+  const EncodeFn encode = tensor_map_encoder();
+  if (encode == nullptr) return false;
+  const cuuint64_t dims[3] = {cuuint64_t(dh), cuuint64_t(heads), cuuint64_t(rows)};
+  const cuuint64_t strides[2] = {cuuint64_t(head) * 2, cuuint64_t(row) * 2};
+  const cuuint32_t box[3] = {64, 1, kPtTile}, steps[3] = {1, 1, 1};
+  return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int DH>
+adore_status_t attention_tc(const PackedParams& p, const void* q, const void* k, const void* v, void* out, float* lse, cudaStream_t st) {
+  const unsigned grid = tile_grid(p, 2 * kPtTile, p.H);
+  if (grid == 0) return ADORE_ERR_UNSUPPORTED;
+  PtMaps maps;
+  if (!packed_map(&maps.q, q, p.q_row, p.q_head, p.total, p.H, DH) || !packed_map(&maps.k, k, p.k_row, p.k_head, p.total, p.Hk, DH) ||
+      !packed_map(&maps.v, v, p.v_row, p.v_head, p.total, p.Hk, DH))
+    return ADORE_ERR_CUDA;
+  if (!allow_smem(prompt_attention_tc_kernel<DH>, PtSmem<DH>::kTotal)) return ADORE_ERR_CUDA;
+  prompt_attention_tc_kernel<DH><<<grid, kPtThreads, PtSmem<DH>::kTotal, st>>>(maps, p, static_cast<__nv_bfloat16*>(out), lse);
+  return launched();
+}
+
 adore_status_t check_q4(const adore_q4_t* c) {
   if (!c || c->struct_size != sizeof(adore_q4_t) || c->batch < 1 || c->capacity < 1) return ADORE_ERR_INVALID_ARG;
   const adore_status_t st = check_heads(c->n_heads, c->n_kv_heads, c->head_dim, c->dtype, c->scale);
@@ -176,7 +217,9 @@ adore_status_t adore_prompt_attention(const adore_prompt_t* shape, const int32_t
   if (shape->total == 0) return ADORE_OK;
   if (!q || !k || !v || !out || !aligned16({q, k, v, out}) || !aligned4({lse})) return ADORE_ERR_INVALID_ARG;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  return ADORE_BY_TYPE(shape->dtype, shape->head_dim, attention_simt, p, q, k, v, out, lse, st);
+  if (shape->dtype == ADORE_BF16)
+    return shape->head_dim == 64 ? attention_tc<64>(p, q, k, v, out, lse, st) : attention_tc<128>(p, q, k, v, out, lse, st);
+  return shape->head_dim == 64 ? attention_simt<float, 64>(p, q, k, v, out, lse, st) : attention_simt<float, 128>(p, q, k, v, out, lse, st);
 }
 
 adore_status_t adore_prompt_weights(const adore_prompt_t* shape, const int32_t* seq_start, const void* q, const void* k,

@@ -7,6 +7,7 @@
 #include "evict.cuh"
 #include "prompt_attention.cuh"
 #include "prompt_attention_tc.cuh"
+#include "prompt_weights_tc.cuh"
 #include "q4_attention.cuh"
 
 using namespace adore;
@@ -82,6 +83,19 @@ unsigned tile_grid(const PackedParams& p, int block, int heads) {
   return n <= kMaxGrid ? unsigned(n) : 0u;
 }
 
+// SMs of the current device.
+int sm_count() {
+  static int known[64] = {};
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) { cudaGetLastError(); return 148; }
+  if (known[dev] == 0) {
+    int n = 0;
+    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 1) { cudaGetLastError(); return 148; }
+    known[dev] = n;
+  }
+  return known[dev];
+}
+
 adore_status_t launched() { return cudaGetLastError() == cudaSuccess ? ADORE_OK : ADORE_ERR_CUDA; }
 
 template <typename K>
@@ -140,14 +154,26 @@ bool packed_map(CUtensorMap* map, const void* base, int64_t row, int64_t head, i
 
 template <int DH>
 adore_status_t attention_tc(const PackedParams& p, const void* q, const void* k, const void* v, void* out, float* lse, cudaStream_t st) {
-  const unsigned grid = tile_grid(p, 2 * kPtTile, p.H);
-  if (grid == 0) return ADORE_ERR_UNSUPPORTED;
+  const int64_t works = (int64_t(p.total) / (2 * kPtTile) + p.S) * p.H;
+  const unsigned grid = unsigned(std::min<int64_t>(works, sm_count()));
   PtMaps maps;
   if (!packed_map(&maps.q, q, p.q_row, p.q_head, p.total, p.H, DH) || !packed_map(&maps.k, k, p.k_row, p.k_head, p.total, p.Hk, DH) ||
       !packed_map(&maps.v, v, p.v_row, p.v_head, p.total, p.Hk, DH))
     return ADORE_ERR_CUDA;
   if (!allow_smem(prompt_attention_tc_kernel<DH>, PtSmem<DH>::kTotal)) return ADORE_ERR_CUDA;
   prompt_attention_tc_kernel<DH><<<grid, kPtThreads, PtSmem<DH>::kTotal, st>>>(maps, p, static_cast<__nv_bfloat16*>(out), lse);
+  return launched();
+}
+
+template <int DH>
+adore_status_t weights_tc(const PackedParams& p, const void* q, const void* k, const float* lse, int window, float* acc, cudaStream_t st) {
+  const int64_t works = (int64_t(p.total) / kPtTile + p.S) * p.Hk;
+  const unsigned grid = unsigned(std::min<int64_t>(works, sm_count()));
+  PwMaps maps;
+  if (!packed_map(&maps.q, q, p.q_row, p.q_head, p.total, p.H, DH) || !packed_map(&maps.k, k, p.k_row, p.k_head, p.total, p.Hk, DH))
+    return ADORE_ERR_CUDA;
+  if (!allow_smem(prompt_weights_tc_kernel<DH>, PwSmem<DH>::kTotal)) return ADORE_ERR_CUDA;
+  prompt_weights_tc_kernel<DH><<<grid, kPwThreads, PwSmem<DH>::kTotal, st>>>(maps, p, lse, window, acc);
   return launched();
 }
 
@@ -231,7 +257,10 @@ adore_status_t adore_prompt_weights(const adore_prompt_t* shape, const int32_t* 
   if (shape->total == 0) return ADORE_OK;
   if (!q || !k || !lse || !acc || !aligned16({q, k}) || !aligned4({lse, acc})) return ADORE_ERR_INVALID_ARG;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  return ADORE_BY_TYPE(shape->dtype, shape->head_dim, weights_simt, p, q, k, lse, window, acc, st);
+  if (shape->dtype == ADORE_BF16)
+    return shape->head_dim == 64 ? weights_tc<64>(p, q, k, lse, window, acc, st) : weights_tc<128>(p, q, k, lse, window, acc, st);
+  return shape->head_dim == 64 ? weights_simt<float, 64>(p, q, k, lse, window, acc, st)
+                               : weights_simt<float, 128>(p, q, k, lse, window, acc, st);
 }
 
 size_t adore_q4_bytes(const adore_q4_t* shape) {

@@ -2,21 +2,24 @@
 //
 //   S = Q K^T,  P = exp(scale (S - m)),  O = P V / rowsum P,  lse = scale m + log rowsum P
 //
-// One CTA owns 256 consecutive query rows of one head as two tiles of 128 and walks over the blocks of 128 keys up to the
-// diagonal; both tiles use a block while it is in shared memory. Roles (12 warps, two of them idle, one CTA per SM):
-//   warp 8     producer: Q tiles once, then K and V blocks by TMA (128-byte swizzle) through a ring of shared-memory stages
-//   warp 9     one thread issues the MMAs: S_t = Q_t K^T (both operands in shared memory), O_t += P_t V (P_t in TMEM, V as
-//              an N-major operand, so that no transposed copy is needed)
-//   warps 0-3  softmax of tile 0, warps 4-7 of tile 1: one row per thread, the whole row of 128 logits in registers
-// While one tile's softmax runs, the tensor core works on the other tile: the issue order per block is P V of tile 0, next S
-// of tile 0, P V of tile 1, next S of tile 1. P is written over S as bfloat16; the MMAs execute in order, so the next S cannot
-// overtake the P V that reads it. TMEM: 2 x 128 columns of S / P and 2 x dh of O.
+// One CTA works on 256 consecutive query rows of one head as two tiles of 128 and walks over the keys up to the diagonal, 64 at
+// a time; both tiles use a block of 128 keys and values while it is in shared memory. Roles (11 warps, one CTA per SM):
+//   warp 8     producer: Q tiles, then K and V blocks by TMA (128-byte swizzle) through a ring of shared-memory stages
+//   warps 9-10 issue the MMAs of a tile each: S_t = Q_t K^T (both operands in shared memory), O_t += P_t V (P_t in TMEM, V
+//              as an N-major operand, so that no transposed copy is needed)
+//   warps 0-3  softmax of tile 0, warps 4-7 of tile 1: one row per thread
+// TMEM: per tile two buffers of 64 columns for S and dh columns for O. P is written over S as bfloat16. The logits of 64 keys
+// are computed while the softmax works on the 64 before them: as soon as the weights of step i are there, its issuer sends
+// O += P_i V and, behind it into the same buffer, S of step i + 2; the MMAs execute in order. (With one buffer of 128 columns a
+// softmax warp waited 1700 of every 3700 cycles for its next logits: the hand-over there and back costs 700 besides the two
+// products.) The CTAs are persistent: the producer looks up the next piece of work and loads its Q while the current one runs,
+// and the next S products are issued while the softmax warps still write the last rows out.
 //
 // The row maximum that the weights refer to is raised only when a row's maximum has grown by more than 2^8 (weights of up to 256
 // lose nothing in float32 sums and bfloat16 operands); O then has to be rescaled in TMEM, which is rare after the first
 // blocks. A weight is rounded to bfloat16 for the product with V (half a step, 2^-8 of its value), the sum takes it unrounded.
 //
-// Only the last block of a tile (the diagonal) needs a mask: tiles and blocks are aligned alike. Rows behind the end of the
+// Only the last 128 keys of a tile (the diagonal) need a mask: tiles and blocks are aligned alike. Rows behind the end of the
 // sequence belong to other sequences or to nobody: their logits are masked there, and their V rows are zeroed in shared memory,
 // because 0 times an infinity or NaN would not be 0.
 #pragma once
@@ -27,15 +30,15 @@
 namespace adore {
 
 constexpr int kPtTile = 128;
-constexpr int kPtThreads = 384;           // two softmax warpgroups, one with the producer and the issuer
-// 384 threads x 168 registers at launch = 64512; 256 x 208 + 128 x 80 = 63488
-constexpr int kPtRegsSoftmax = 208, kPtRegsOther = 80;
+constexpr int kPtStep = 64;               // keys per step of the softmax
+constexpr int kPtThreads = 352;
 
 template <int DH>
 struct PtSmem {
-  static constexpr int kStages = DH == 128 ? 5 : 8;
+  static constexpr int kStages = DH == 128 ? 4 : 8;
   static constexpr int kTileBytes = kPtTile * DH * 2;
-  static constexpr size_t kTotal = size_t(2 + kStages) * kTileBytes + 256 + 1024;    // + barriers + alignment slack
+  static constexpr int kStageOutBytes = 8 * 32 * 128;      // 32 rows x 64 elements per softmax warp on their way out
+  static constexpr size_t kTotal = size_t(2 + kStages) * kTileBytes + kStageOutBytes + 512 + 1024;    // + barriers + alignment slack
 };
 
 __device__ __forceinline__ float pt_exp2(float x) {
@@ -75,269 +78,367 @@ __device__ __forceinline__ void pt_load_tile(void* dst, const CUtensorMap* map, 
   for (int i = 0; i < DH / 64; ++i) tc_tma_load_3d(static_cast<unsigned char*>(dst) + i * (kPtTile * 128), map, 64 * i, head, row, bar);
 }
 
-// D = A B^T for two K-major tiles of 128 rows x DH.
+// S = Q K^T for a tile of 128 queries and the 64 keys of one half of a key block, both K-major.
 template <int DH>
-__device__ __forceinline__ void pt_mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc) {
+__device__ __forceinline__ void pt_mma_s(uint32_t d, const void* q_tile, const void* k_tile, int half, uint32_t idesc) {
+  const uint64_t a = tc_smem_desc(q_tile), b = tc_smem_desc(k_tile) + uint64_t(half * (kPtStep * 128 / 16));
 #pragma unroll
   for (int k = 0; k < DH / 16; ++k) {
     const uint64_t at = uint64_t((k / 4) * (kPtTile * 128 / 16) + (k % 4) * 2);
-    tc_mma_bf16(d, a + at, b + at, idesc, k != 0 ? 1u : 0u);
+    tc_mma_bf16_warp(d, a + at, b + at, idesc, k != 0 ? 1u : 0u);
   }
+}
+// O += P V for 64 keys: 16 keys are 8 columns of P and two groups of 8 rows of V.
+template <int DH>
+__device__ __forceinline__ void pt_mma_o(uint32_t d, uint32_t p_tmem, const void* v_tile, int half, uint32_t idesc, bool first) {
+  const uint64_t b = tc_smem_desc_n(v_tile, kPtTile * 128) + uint64_t(half * (kPtStep * 128 / 16));
+#pragma unroll
+  for (int k = 0; k < kPtStep / 16; ++k) tc_mma_bf16_ts_warp(d, p_tmem + 8 * k, b + uint64_t(128 * k), idesc, first && k == 0 ? 0u : 1u);
 }
 
 struct PtMaps { CUtensorMap q, k, v; };
+
+// What a CTA works on next; `found` 0 ends it.
+struct PtWork { int start, len, index, h, found; };
+
+// Weights 2^(c s + off) of a row's 64 logits: stored as bfloat16 over the logits, summed unrounded.
+__device__ __forceinline__ float pt_weights_row(const uint32_t (&s)[2][32], float c, float off, uint32_t s_at) {
+  const unsigned long long c2 = pt_pack(c, c), off2 = pt_pack(off, off);
+  unsigned long long sum[2] = {0ull, 0ull};
+  uint32_t w[32];
+#pragma unroll
+  for (int e = 0; e < 32; ++e) {
+    const uint32_t* x = &s[e / 16][2 * (e % 16)];
+    const unsigned long long y = pt_fma2(pt_pack(__uint_as_float(x[0]), __uint_as_float(x[1])), c2, off2);
+    float a, b;
+    pt_unpack(y, a, b);
+    a = pt_exp2(a);
+    b = pt_exp2(b);
+    sum[e & 1] = pt_add2(sum[e & 1], pt_pack(a, b));
+    w[e] = pt_bf16x2(a, b);
+  }
+  tc_st_32x32(s_at, w);
+  float a, b;
+  pt_unpack(pt_add2(sum[0], sum[1]), a, b);
+  return a + b;
+}
+__device__ __forceinline__ float pt_row_max(const uint32_t (&s)[2][32]) {
+  float tops[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    tops[i] = __uint_as_float(s[i / 2][16 * (i % 2)]);
+#pragma unroll
+    for (int e = 1; e < 16; ++e) tops[i] = fmaxf(tops[i], __uint_as_float(s[i / 2][16 * (i % 2) + e]));
+  }
+  return fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+}
+
+// Steps of tile t of a piece of work: up to the tile's own rows and the sequence's end; 0 if it has no tile t.
+__device__ __forceinline__ int pt_steps(const PtWork& w, int t) {
+  const int row0 = (2 * w.index + t) * kPtTile;
+  return row0 < w.len ? (min(row0 + kPtTile, w.len) + kPtStep - 1) / kPtStep : 0;
+}
 
 template <int DH>
 __global__ void __launch_bounds__(kPtThreads, 1)
 prompt_attention_tc_kernel(const __grid_constant__ PtMaps maps, const PackedParams p, __nv_bfloat16* out, float* lse) {
   using S = PtSmem<DH>;
-  constexpr int kStages = S::kStages;
+  constexpr uint32_t kStages = S::kStages;
   extern __shared__ __align__(1024) unsigned char pt_smem_raw[];
   unsigned char* base = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(pt_smem_raw) + 1023) & ~uintptr_t(1023));
   unsigned char* q_tiles = base;
   unsigned char* ring = base + 2 * S::kTileBytes;
-  uint64_t* bars = reinterpret_cast<uint64_t*>(ring + size_t(kStages) * S::kTileBytes);
+  unsigned char* stage_out = ring + size_t(kStages) * S::kTileBytes;
+  uint64_t* bars = reinterpret_cast<uint64_t*>(stage_out + S::kStageOutBytes);
   uint64_t* kv_full = bars;
   uint64_t* kv_empty = kv_full + kStages;
-  uint64_t* q_full = kv_empty + kStages;      // per tile
-  uint64_t* s_full = q_full + 2;              // logits ready (and every earlier MMA done)
-  uint64_t* p_full = s_full + 2;              // weights stored, O rescaled if needed
-  uint64_t* o_full = p_full + 2;              // last product done
-  uint64_t* drain = o_full + 2;               // after a wait that ran out: every issued MMA done
-  __shared__ PackedTile tile;
-  __shared__ int found, s_abort;
+  uint64_t* q_full = kv_empty + kStages;      // [tile]
+  uint64_t* q_empty = q_full + 2;             // [tile] last S product of the tile done
+  uint64_t* s_full = q_empty + 2;             // [tile][buffer] logits ready
+  uint64_t* p_full = s_full + 4;              // [tile][buffer] weights stored, O rescaled if needed
+  uint64_t* o_done = p_full + 4;              // [tile][step & 1] product with V done
+  uint64_t* o_empty = o_done + 4;             // [tile] O has been read
+  uint64_t* work_full = o_empty + 2;          // the next piece of work is known
+  uint64_t* work_empty = work_full + 2;       // the issuers and the softmax warps have read it
+  uint64_t* drain = work_empty + 2;           // [tile] after a wait that ran out: every issued MMA done
+  __shared__ PtWork works[2];
+  __shared__ int s_abort;
   __shared__ uint32_t tmem_slot;
   volatile int* abort_flag = &s_abort;
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int h = blockIdx.x % p.H, g = h / p.group;
   if (threadIdx.x == 0) {
-    for (int i = 0; i < kStages; ++i) { tc_mbar_init(&kv_full[i], 1u); tc_mbar_init(&kv_empty[i], 1u); }
+    for (uint32_t i = 0; i < kStages; ++i) { tc_mbar_init(&kv_full[i], 1u); tc_mbar_init(&kv_empty[i], 2u); }
     for (int t = 0; t < 2; ++t) {
       tc_mbar_init(&q_full[t], 1u);
-      tc_mbar_init(&s_full[t], 1u);
-      tc_mbar_init(&p_full[t], 4u);
-      tc_mbar_init(&o_full[t], 1u);
+      tc_mbar_init(&q_empty[t], 1u);
+      for (int b = 2 * t; b < 2 * t + 2; ++b) { tc_mbar_init(&s_full[b], 1u); tc_mbar_init(&p_full[b], 4u); tc_mbar_init(&o_done[b], 1u); }
+      tc_mbar_init(&o_empty[t], 4u);
+      tc_mbar_init(&work_full[t], 1u);
+      tc_mbar_init(&work_empty[t], 10u);
+      tc_mbar_init(&drain[t], 1u);
     }
-    tc_mbar_init(drain, 1u);
     s_abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
-  if (warp == 8) {
-    PackedTile t{};
-    const bool ok = find_packed_tile<2 * kPtTile>(p.seq_start, p.S, p.total, blockIdx.x / p.H, p.err, t);
-    if (lane == 0) { tile = t; found = ok; }
-  }
-  __syncthreads();
-  if (!found) return;
   if (warp == 9) { __syncwarp(); tc_alloc(&tmem_slot, 512); }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = tmem_slot;
-  const uint32_t o_cols = 256;                // S of tile t at column 128 t, O of tile t at 256 + DH t
-  const int len = tile.len, q0 = tile.index * 2 * kPtTile;
-  const bool two = len > q0 + kPtTile;
-  const int n0 = 2 * tile.index + 1, n1 = two ? n0 + 1 : 0, blocks = two ? n1 : n0;
+  const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_slot, 0);
+  const uint32_t o_cols = 256;                // S of tile t, buffer b at column 128 t + 64 b, O of tile t at 256 + DH t
 
-  int issued = 0;                             // producer: ring loads issued
+  uint32_t issued = 0, q0_issued = 0, q1_issued = 0;      // producer: loads issued
+  auto give_up = [&]() { if (!*abort_flag) { if (p.err != nullptr) set_error(p.err, ERRW_TIMEOUT); *abort_flag = 1; } };
+  // every reader takes a copy and hands the slot back
+  auto next_work = [&](uint32_t it, PtWork& w) {
+    if (!tc_mbar_poll_warp(&work_full[it & 1], (it >> 1) & 1u, abort_flag)) return false;
+    w = works[it & 1];
+    __syncwarp();
+    if (lane == 0) tc_mbar_arrive(&work_empty[it & 1]);
+    return true;
+  };
 
-  if (warp >= 8) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kPtRegsOther));
-    if (warp == 8) {
-      // ---------------- producer ----------------
-      if (lane == 0) {
-        bool ok = true;
-        pt_load_tile<DH>(q_tiles, &maps.q, h, tile.start + q0, &q_full[0]);
-        // K0 V0 K1 V1 ..
-        for (int i = 0; i < 2 * blocks; ++i) {
-          const int stage = i % kStages;
-          if (i >= kStages && !tc_mbar_wait(&kv_empty[stage], uint32_t(i / kStages - 1) & 1u, abort_flag)) { ok = false; break; }
-          pt_load_tile<DH>(ring + size_t(stage) * S::kTileBytes, (i & 1) ? &maps.v : &maps.k, g, tile.start + (i >> 1) * kPtTile, &kv_full[stage]);
-          issued = i + 1;
-          if (i == 0 && two) pt_load_tile<DH>(q_tiles + S::kTileBytes, &maps.q, h, tile.start + q0 + kPtTile, &q_full[1]);
+  if (warp == 8) {
+    // ---------------- producer; also looks up the work, one piece ahead ----------------
+    bool ok = true;
+    PtWork w{};
+    auto look_up = [&](uint32_t it) {
+      const long long i = (long long)it * gridDim.x + ((it & 1) ? gridDim.x - 1 - blockIdx.x : blockIdx.x);     // back and forth: even shares
+      PackedTile t{};
+      w.found = i / p.H < 0x7fffffff && find_packed_tile<2 * kPtTile>(p.seq_start, p.S, p.total, int(i / p.H), it == 0 ? p.err : nullptr, t);
+      w.start = t.start; w.len = t.len; w.index = t.index; w.h = int(i % p.H);
+      if (it >= 2 && !tc_mbar_poll_warp(&work_empty[it & 1], ((it >> 1) - 1) & 1u, abort_flag)) return false;
+      if (lane == 0) { works[it & 1] = w; tc_mbar_arrive(&work_full[it & 1]); }
+      __syncwarp();
+      return true;
+    };
+    ok = look_up(0);
+    for (uint32_t it = 0; ok && w.found; ++it) {
+      const PtWork cur = w;
+      const int q0 = cur.index * 2 * kPtTile, g = cur.h / p.group;
+      const bool two = cur.len > q0 + kPtTile;
+      const int loads = 2 * ((max(pt_steps(cur, 0), pt_steps(cur, 1)) + 1) / 2);
+      // Q0 K0 Q1 V0 K1 V1 ..
+      for (int i = 0; i < loads && ok; ++i) {
+        if (i == 0) {
+          if (q0_issued > 0 && !tc_mbar_poll_warp(&q_empty[0], (q0_issued - 1) & 1u, abort_flag)) { ok = false; break; }
+          if (lane == 0) pt_load_tile<DH>(q_tiles, &maps.q, cur.h, cur.start + q0, &q_full[0]);
+          ++q0_issued;
+        } else if (i == 1 && two) {
+          if (q1_issued > 0 && !tc_mbar_poll_warp(&q_empty[1], (q1_issued - 1) & 1u, abort_flag)) { ok = false; break; }
+          if (lane == 0) pt_load_tile<DH>(q_tiles + S::kTileBytes, &maps.q, cur.h, cur.start + q0 + kPtTile, &q_full[1]);
+          ++q1_issued;
         }
-        if (!ok && !*abort_flag) { if (p.err != nullptr) set_error(p.err, ERRW_TIMEOUT); *abort_flag = 1; }
+        const uint32_t stage = issued % kStages, use = issued / kStages;
+        if (use > 0 && !tc_mbar_poll_warp(&kv_empty[stage], (use - 1) & 1u, abort_flag)) { ok = false; break; }
+        if (lane == 0)
+          pt_load_tile<DH>(ring + size_t(stage) * S::kTileBytes, (i & 1) ? &maps.v : &maps.k, g, cur.start + (i >> 1) * kPtTile, &kv_full[stage]);
+        ++issued;
+        __syncwarp();
+        if (i == min(loads, int(kStages)) - 1) ok = look_up(it + 1);     // beside the first blocks' arrival
       }
-    } else if (warp == 9) {
-      // ---------------- MMA issuer ----------------
-      const uint32_t idesc_s = tc_idesc(kPtTile, kPtTile) | (p.scale < 0.f ? kTcIdescNegA : 0u);     // the softmax then takes |scale|
-      constexpr uint32_t idesc_o = tc_idesc(kPtTile, DH) | kTcIdescBN;
-      bool ok = true;
-      const int tail = (len - 1) / kPtTile, tail_rows = len - tail * kPtTile;      // last block of the sequence and its rows
-      for (int t = 0; t < (two ? 2 : 1) && ok; ++t) {
-        ok = tc_mbar_wait_warp(&q_full[t], 0u, abort_flag) && (t == 1 || tc_mbar_wait_warp(&kv_full[0], 0u, abort_flag));
+    }
+    if (!ok && lane == 0) give_up();
+  } else if (warp >= 9) {
+    // ---------------- MMA issuer of tile `t` ----------------
+    const int t = warp - 9;
+    const uint32_t idesc_s = tc_idesc(kPtTile, kPtStep) | (p.scale < 0.f ? kTcIdescNegA : 0u);     // the softmax then takes |scale|
+    constexpr uint32_t idesc_o = tc_idesc(kPtTile, DH) | kTcIdescBN;
+    const uint32_t s_base = tmem + 128 * t, o_base = tmem + o_cols + DH * t;
+    bool ok = true;
+    // S products and P V products issued so far, tiles finished, ring places of the work before
+    uint32_t used = 0, s_count = 0, o_count = 0, tiles_done = 0;
+    for (uint32_t it = 0; ok; ++it) {
+      PtWork w;
+      if (!next_work(it, w)) { ok = false; break; }
+      w.len = __shfl_sync(0xffffffffu, w.len, 0);                // alike in all lanes, and known to be
+      w.index = __shfl_sync(0xffffffffu, w.index, 0);
+      if (!w.found) break;
+      const int n = pt_steps(w, t), blocks = (max(pt_steps(w, 0), pt_steps(w, 1)) + 1) / 2;
+      const int tail = (w.len - 1) / kPtTile, tail_rows = w.len - tail * kPtTile;      // last block of the sequence and its rows
+      // ring places of this work: K_j at used + 2 j, V_j at used + 2 j + 1
+      auto place = [&](uint32_t i) { return ring + size_t((used + i) % kStages) * S::kTileBytes; };
+      auto loaded = [&](uint32_t i) { return tc_mbar_poll_warp(&kv_full[(used + i) % kStages], ((used + i) / kStages) & 1u, abort_flag); };
+      auto release = [&](uint32_t i) { tc_commit_warp(&kv_empty[(used + i) % kStages]); };      // both issuers do, after their last use
+      auto issue_s = [&](int i) {
+        const uint32_t b = s_count & 1u;
+        pt_mma_s<DH>(s_base + 64 * b, q_tiles + t * S::kTileBytes, place(2 * (i >> 1)), i & 1, idesc_s);
+        tc_commit_warp(&s_full[2 * t + b]);
+        ++s_count;
+      };
+      ok = loaded(0);
+      if (!ok) break;
+      if (n > 0) {
+        ok = tc_mbar_poll_warp(&q_full[t], tiles_done & 1u, abort_flag);
         if (!ok) break;
         tc_fence_after();
-        if (lane == 0) {
-          pt_mma_ss<DH>(tmem + 128 * t, tc_smem_desc(q_tiles + t * S::kTileBytes), tc_smem_desc(ring), idesc_s);
-          tc_commit(&s_full[t]);
-        }
-        __syncwarp();
+        issue_s(0);
+        if (n > 1) issue_s(1);
+        if (n <= 2) tc_commit_warp(&q_empty[t]);
       }
-      if (ok && lane == 0) tc_commit(&kv_empty[0]);
-      for (int j = 0; j < blocks && ok; ++j) {
-        const int vi = 2 * j + 1, vs = vi % kStages, ki = vi + 1, ks = ki % kStages;
-        unsigned char* v_tile = ring + size_t(vs) * S::kTileBytes;
-        if (!tc_mbar_wait_warp(&kv_full[vs], uint32_t(vi / kStages) & 1u, abort_flag)) { ok = false; break; }
-        if (j == tail && tail_rows < kPtTile) {
-          constexpr int kPieces = 8 * (DH / 64);                 // 16-byte pieces of a row, in boxes of 8
-          for (int i = lane; i < (kPtTile - tail_rows) * kPieces; i += 32) {
-            const int r = tail_rows + i / kPieces, c = i % kPieces;
-            *reinterpret_cast<uint4*>(v_tile + (c / 8) * (kPtTile * 128) + r * 128 + (c % 8) * 16) = make_uint4(0u, 0u, 0u, 0u);
-          }
-          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-          __syncwarp();
-        }
-        for (int t = 0; t < 2; ++t) {
-          const int n = t == 0 ? n0 : n1;
-          if (j >= n) continue;
-          if (!tc_mbar_wait_warp(&p_full[t], uint32_t(j) & 1u, abort_flag)) { ok = false; break; }
-          if (j + 1 < n && !tc_mbar_wait_warp(&kv_full[ks], uint32_t(ki / kStages) & 1u, abort_flag)) { ok = false; break; }
-          tc_fence_after();
-          if (lane == 0) {
-            const uint64_t vd = tc_smem_desc_n(v_tile, kPtTile * 128);
-  #pragma unroll
-            for (int k = 0; k < kPtTile / 16; ++k)               // 16 keys: 8 columns of P, two groups of 8 rows of V
-              tc_mma_bf16_ts(tmem + o_cols + DH * t, tmem + 128 * t + 8 * k, vd + uint64_t(128 * k), idesc_o, (j | k) != 0 ? 1u : 0u);
-            if (j + 1 < n) {
-              pt_mma_ss<DH>(tmem + 128 * t, tc_smem_desc(q_tiles + t * S::kTileBytes), tc_smem_desc(ring + size_t(ks) * S::kTileBytes), idesc_s);
-              tc_commit(&s_full[t]);
-            } else {
-              tc_commit(&o_full[t]);
+      release(0);
+      for (int i = 0; i < n; ++i) {
+        const int j = i >> 1;
+        if ((i & 1) == 0) {
+          if (!loaded(2 * j + 1) || (i + 2 < n && !loaded(2 * j + 2))) { ok = false; break; }
+          if (j == tail && tail_rows < kPtTile) {                // (both issuers may do this: the same zeros)
+            constexpr int kPieces = 8 * (DH / 64);               // 16-byte pieces of a row, in boxes of 8
+            unsigned char* v_tile = place(2 * j + 1);
+            for (int x = lane; x < (kPtTile - tail_rows) * kPieces; x += 32) {
+              const int r = tail_rows + x / kPieces, c = x % kPieces;
+              *reinterpret_cast<uint4*>(v_tile + (c / 8) * (kPtTile * 128) + r * 128 + (c % 8) * 16) = make_uint4(0u, 0u, 0u, 0u);
             }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
           }
-          __syncwarp();
+          if (i == 0 && tiles_done > 0 && !tc_mbar_poll_warp(&o_empty[t], (tiles_done - 1) & 1u, abort_flag)) { ok = false; break; }
         }
-        if (ok && lane == 0) {
-          tc_commit(&kv_empty[vs]);
-          if (j + 1 < blocks) tc_commit(&kv_empty[ks]);
-        }
+        const uint32_t b = o_count & 1u;
+        if (!tc_mbar_poll_warp(&p_full[2 * t + b], (o_count >> 1) & 1u, abort_flag)) { ok = false; break; }
+        tc_fence_after();
+        pt_mma_o<DH>(o_base, s_base + 64 * b, place(2 * j + 1), i & 1, idesc_o, i == 0);
+        tc_commit_warp(&o_done[2 * t + b]);
+        ++o_count;
+        if (i + 2 < n) issue_s(i + 2);
+        if (i + 3 == n) tc_commit_warp(&q_empty[t]);
+        if ((i & 1) == 1 || i == n - 1) release(2 * j + 1);
+        if (i + 2 < n && ((i & 1) == 1 || i + 2 == n - 1)) release(2 * j + 2);
       }
-      if (!ok) {
-        if (lane == 0) {
-          if (!*abort_flag) { if (p.err != nullptr) set_error(p.err, ERRW_TIMEOUT); *abort_flag = 1; }
-          tc_commit(drain);
+      if (!ok) break;
+      // Blocks that only the other tile uses. A stage is handed back only after its load has arrived: the arrival says that both
+      // issuers handed back its use before, so the two arrivals of a use cannot mix with those of the next.
+      for (int j = (n + 1) / 2; j < blocks && ok; ++j) {
+        if (j > 0) {
+          ok = loaded(2 * j);
+          if (ok) release(2 * j);
         }
-        int never = 0;
-        tc_mbar_wait_warp(drain, 0u, &never);
+        ok = ok && loaded(2 * j + 1);
+        if (ok) release(2 * j + 1);
       }
+      if (!ok) break;
+      if (n > 0) ++tiles_done;
+      used += 2 * blocks;
+    }
+    if (!ok) {
+      if (lane == 0) give_up();
+      __syncwarp();
+      tc_commit_warp(&drain[t]);
+      int never = 0;
+      tc_mbar_poll_warp(&drain[t], 0u, &never);
     }
   } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kPtRegsSoftmax));
     // ---------------- softmax of tile `t`, one row per thread ----------------
     const int t = warp >> 2, quarter = warp & 3;
-    const int n = t == 0 ? n0 : n1;
-    const int r = quarter * 32 + lane, row = q0 + t * kPtTile + r;
+    const int r = quarter * 32 + lane;
     const uint32_t lanes = uint32_t(quarter * 32) << 16;
-    const uint32_t s_at = tmem + lanes + 128 * t, o_at = tmem + lanes + o_cols + DH * t;
-    const float c = fabsf(p.scale) * 1.4426950408889634f;      // logits in units of log 2
-    float m = -INFINITY, l = 0.f;
+    const uint32_t o_at = tmem + lanes + o_cols + DH * t;
+    unsigned char* my_out = stage_out + warp * (32 * 128);
+    const float c = fabsf(p.scale) * 1.4426950408889634f;        // logits in units of log 2
     bool ok = true;
-    for (int j = 0; j < n; ++j) {
-      if (!tc_mbar_wait_warp(&s_full[t], uint32_t(j) & 1u, abort_flag)) { ok = false; break; }
-      tc_fence_after();
-      uint32_t s[4][32];
-      __syncwarp();
+    uint32_t count = 0;                                          // steps done
+    for (uint32_t it = 0; ok; ++it) {
+      PtWork w;
+      if (!next_work(it, w)) { ok = false; break; }
+      if (!w.found) break;
+      const int n = pt_steps(w, t);
+      if (n == 0) continue;
+      const int row0 = (2 * w.index + t) * kPtTile;
+      float m = -INFINITY, l = 0.f;
+      for (int i = 0; i < n; ++i, ++count) {
+        const uint32_t b = count & 1u, s_at = tmem + lanes + 128 * t + 64 * b;
+        if (!tc_mbar_poll_warp(&s_full[2 * t + b], (count >> 1) & 1u, abort_flag)) { ok = false; break; }
+        tc_fence_after();
+        uint32_t s[2][32];
+        __syncwarp();
+        tc_ld_32x32_start(s_at, s[0]);
+        tc_ld_32x32_start(s_at + 32, s[1]);
+        tc_ld_wait(s[0]);
+        tc_ld_wait(s[1]);
+        const int ahead = r - (i * kPtStep - row0);              // keys of this step up to the row's own
+        const bool diagonal = i * kPtStep >= row0;
+        if (diagonal) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) tc_ld_32x32_start(s_at + 32 * i, s[i]);
+          for (int x = 0; x < 2; ++x)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) tc_ld_wait(s[i]);
-      if (j == n - 1) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-          for (int e = 0; e < 32; ++e)
-            if (32 * i + e > r) s[i][e] = 0xff800000u;
-      }
-      float tops[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        tops[i] = __uint_as_float(s[i][0]);
-#pragma unroll
-        for (int e = 1; e < 32; ++e) tops[i] = fmaxf(tops[i], __uint_as_float(s[i][e]));
-      }
-      const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
-      const bool raise = (top - m) * c > 8.f;                  // also the first block: m = -inf
-      if (__any_sync(0xffffffffu, raise)) {
-        const float f = raise ? pt_exp2((m - top) * c) : 1.f;
-        if (raise) m = top;
-        l *= f;
-        if (j > 0) {
+            for (int e = 0; e < 32; ++e)
+              if (32 * x + e > ahead) s[x][e] = 0xff800000u;
+        }
+        const float top = pt_row_max(s);
+        const bool raise = (top - m) * c > 8.f;                  // also the first step: m = -inf
+        if (__any_sync(0xffffffffu, raise)) {
+          const float f = raise ? pt_exp2((m - top) * c) : 1.f;
+          if (raise) m = top;
+          l *= f;
+          if (i > 0) {
+            if (!tc_mbar_poll_warp(&o_done[2 * t + ((count - 1) & 1u)], ((count - 1) >> 1) & 1u, abort_flag)) { ok = false; break; }
+            tc_fence_after();
 #pragma unroll 1
-          for (int i = 0; i < DH / 32; ++i) {
-            uint32_t o[32];
-            tc_ld_32x32_start(o_at + 32 * i, o);
-            tc_ld_wait(o);
+            for (int x = 0; x < DH / 32; ++x) {
+              uint32_t o[32];
+              tc_ld_32x32_start(o_at + 32 * x, o);
+              tc_ld_wait(o);
 #pragma unroll
-            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
-            tc_st_32x32(o_at + 32 * i, o);
+              for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+              tc_st_32x32(o_at + 32 * x, o);
+            }
           }
         }
+        l += pt_weights_row(s, c, -m * c, s_at);
+        tc_st_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) tc_mbar_arrive(&p_full[2 * t + b]);
       }
-      const unsigned long long c2 = pt_pack(c, c), mc2 = pt_pack(-m * c, -m * c);
-      unsigned long long sum[2] = {0ull, 0ull};
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        uint32_t w[32];
-#pragma unroll
-        for (int e = 0; e < 32; ++e) {
-          const uint32_t* x = &s[2 * i + e / 16][2 * (e % 16)];
-          const unsigned long long y = pt_fma2(pt_pack(__uint_as_float(x[0]), __uint_as_float(x[1])), c2, mc2);
-          float a, b;
-          pt_unpack(y, a, b);
-          a = pt_exp2(a);
-          b = pt_exp2(b);
-          sum[e & 1] = pt_add2(sum[e & 1], pt_pack(a, b));
-          w[e] = pt_bf16x2(a, b);
-        }
-        tc_st_32x32(s_at + 32 * i, w);
-      }
-      float a, b;
-      pt_unpack(pt_add2(sum[0], sum[1]), a, b);
-      l += a + b;
-      tc_st_wait();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) tc_mbar_arrive(&p_full[t]);
-    }
-    if (n > 0 && ok) ok = tc_mbar_wait_warp(&o_full[t], 0u, abort_flag);
-    if (n > 0 && ok) {
+      if (!ok || !tc_mbar_poll_warp(&o_done[2 * t + ((count - 1) & 1u)], ((count - 1) >> 1) & 1u, abort_flag)) { ok = false; break; }
       tc_fence_after();
       const float inv = 1.f / l;
-      const bool mine = row < len;
-      __nv_bfloat16* dst = out + (tile.start + row) * p.out_row + h * p.out_head;
-#pragma unroll 1
-      for (int i = 0; i < DH / 32; ++i) {
-        uint32_t o[32];
+      // 64 elements at a time through shared memory, so that 8 lanes write 128 consecutive bytes of a row
+#pragma unroll
+      for (int x = 0; x < DH / 64; ++x) {
+        uint32_t o[2][32];
         __syncwarp();
-        tc_ld_32x32_start(o_at + 32 * i, o);
-        tc_ld_wait(o);
-        if (mine) {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            uint32_t w[4];
-#pragma unroll
-            for (int x = 0; x < 4; ++x)
-              w[x] = pt_bf16x2(__uint_as_float(o[8 * e + 2 * x]) * inv, __uint_as_float(o[8 * e + 2 * x + 1]) * inv);
-            reinterpret_cast<uint4*>(dst + 32 * i)[e] = make_uint4(w[0], w[1], w[2], w[3]);
-          }
+        tc_ld_32x32_start(o_at + 64 * x, o[0]);
+        tc_ld_32x32_start(o_at + 64 * x + 32, o[1]);
+        tc_ld_wait(o[0]);
+        tc_ld_wait(o[1]);
+        if (x == DH / 64 - 1) {                                  // O may be overwritten
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) tc_mbar_arrive(&o_empty[t]);
         }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          uint32_t v[4];
+#pragma unroll
+          for (int y = 0; y < 4; ++y)
+            v[y] = pt_bf16x2(__uint_as_float(o[e / 4][8 * (e % 4) + 2 * y]) * inv, __uint_as_float(o[e / 4][8 * (e % 4) + 2 * y + 1]) * inv);
+          *reinterpret_cast<uint4*>(my_out + lane * 128 + ((e ^ (lane & 7)) * 16)) = make_uint4(v[0], v[1], v[2], v[3]);
+        }
+        __syncwarp();
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int rr = 4 * e + (lane >> 3), row = row0 + quarter * 32 + rr;
+          const uint4 v = *reinterpret_cast<const uint4*>(my_out + rr * 128 + (((lane & 7) ^ (rr & 7)) * 16));
+          if (row < w.len)
+            *reinterpret_cast<uint4*>(out + (w.start + row) * p.out_row + w.h * p.out_head + 64 * x + 8 * (lane & 7)) = v;
+        }
+        __syncwarp();
       }
-      if (mine && lse != nullptr) lse[size_t(h) * p.total + tile.start + row] = (m * c + log2f(l)) * 0.6931471805599453f;
+      if (lse != nullptr && row0 + r < w.len) lse[size_t(w.h) * p.total + w.start + row0 + r] = (m * c + log2f(l)) * 0.6931471805599453f;
     }
-    if (!ok && lane == 0 && !*abort_flag) { if (p.err != nullptr) set_error(p.err, ERRW_TIMEOUT); *abort_flag = 1; }
+    if (!ok && lane == 0) give_up();
   }
 
   tc_fence_before();
   __syncthreads();
   if (*abort_flag) {                          // copies in flight have to land before the CTA ends
-    if (warp == 8 && lane == 0) {
+    if (warp == 8) {
       int never = 0;
-      for (int i = max(0, issued - kStages); i < issued; ++i) tc_mbar_wait(&kv_full[i % kStages], uint32_t(i / kStages) & 1u, &never);
-      tc_mbar_wait(&q_full[0], 0u, &never);
-      if (two && issued > 0) tc_mbar_wait(&q_full[1], 0u, &never);
+      for (uint32_t i = issued > kStages ? issued - kStages : 0u; i < issued; ++i) tc_mbar_poll(&kv_full[i % kStages], (i / kStages) & 1u, &never);
+      if (q0_issued > 0) tc_mbar_poll(&q_full[0], (q0_issued - 1) & 1u, &never);
+      if (q1_issued > 0) tc_mbar_poll(&q_full[1], (q1_issued - 1) & 1u, &never);
     }
     __syncthreads();
   }

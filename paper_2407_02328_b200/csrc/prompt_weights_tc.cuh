@@ -1,0 +1,297 @@
+// Attention weight received by every prompt token, on the 5th-generation tensor cores (bfloat16).
+//
+//   acc_j = sum over a group's heads and the queries i >= j (of the last `window`) of exp(scale q_i . k_j - lse_i)
+//
+// A second pass over Q and K: the weights need every row's lse. One piece of work is 128 keys of one key/value head; the
+// CTA holds them as the A operand, so that S = K Q^T has a key per TMEM lane and the sum over the queries runs along the
+// columns of one thread: no exchange between threads, no atomics, the same bits every time. Bound by the exponentials: 16 per
+// cycle and SM against 32 logits per cycle from the tensor core (dh = 128).
+// Roles (11 warps, one persistent CTA per SM):
+//   warp 8     producer: looks up the work, loads K tiles (two, the next piece's early) and streams Q tiles by TMA
+//   warp 9     issues S = K Q^T into one of four TMEM buffers of 128 columns
+//   warp 10    stages -lse log2(e) of the item's 128 queries in shared memory
+//   warps 0-7  two warpgroups that take alternate items: S from TMEM, weights, sums (float32 in an item, float64 over items)
+#pragma once
+
+#include "prompt_attention_tc.cuh"
+
+namespace adore {
+
+constexpr int kPwThreads = 352;
+
+template <int DH>
+struct PwSmem {
+  static constexpr int kStages = DH == 128 ? 4 : 6;
+  static constexpr int kTileBytes = kPtTile * DH * 2;
+  static constexpr size_t kTotal = size_t(2 + kStages) * kTileBytes + 4 * kPtTile * sizeof(float) + kPtTile * sizeof(double) + 512 + 1024;
+};
+
+struct PwMaps { CUtensorMap q, k; };
+
+// What a CTA works on next: keys [128 kb, ..) of a sequence, one key/value head. qb: first query block that counts.
+struct PwWork { int start, len, kb, qb, blocks, g, found; };
+
+// Sum of the weights of 32 queries for one key. `off`: -lse log2(e) of the queries in shared memory.
+template <bool MASKED>
+__device__ __forceinline__ float pw_sum32(const uint32_t (&s)[32], const float* off, float c, int col0, int lo, int hi) {
+  const unsigned long long c2 = pt_pack(c, c);
+  unsigned long long sum[2] = {0ull, 0ull};
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const float4 o = *reinterpret_cast<const float4*>(off + 4 * e);
+    const float os[4] = {o.x, o.y, o.z, o.w};
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const int i = 4 * e + 2 * x;
+      float a, b;
+      pt_unpack(pt_fma2(pt_pack(__uint_as_float(s[i]), __uint_as_float(s[i + 1])), c2, pt_pack(os[2 * x], os[2 * x + 1])), a, b);
+      a = pt_exp2(a);
+      b = pt_exp2(b);
+      if (MASKED) {                           // a select: rows behind the sequence may hold anything
+        if (col0 + i < lo || col0 + i >= hi) a = 0.f;
+        if (col0 + i + 1 < lo || col0 + i + 1 >= hi) b = 0.f;
+      }
+      sum[x] = pt_add2(sum[x], pt_pack(a, b));
+    }
+  }
+  float a, b;
+  pt_unpack(pt_add2(sum[0], sum[1]), a, b);
+  return a + b;
+}
+
+template <int DH>
+__global__ void __launch_bounds__(kPwThreads, 1)
+prompt_weights_tc_kernel(const __grid_constant__ PwMaps maps, const PackedParams p, const float* lse, int window, float* acc) {
+  using S = PwSmem<DH>;
+  constexpr uint32_t kStages = S::kStages;
+  extern __shared__ __align__(1024) unsigned char pw_smem_raw[];
+  unsigned char* base = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(pw_smem_raw) + 1023) & ~uintptr_t(1023));
+  unsigned char* k_tiles = base;
+  unsigned char* ring = base + 2 * S::kTileBytes;
+  float* offs = reinterpret_cast<float*>(ring + size_t(kStages) * S::kTileBytes);      // [4][128]
+  double* partial = reinterpret_cast<double*>(offs + 4 * kPtTile);                     // [128] second warpgroup's sums
+  uint64_t* q_full = reinterpret_cast<uint64_t*>(partial + kPtTile);
+  uint64_t* q_empty = q_full + kStages;
+  uint64_t* k_full = q_empty + kStages;       // [2]
+  uint64_t* k_empty = k_full + 2;             // [2] last product with the tile done
+  uint64_t* s_full = k_empty + 2;             // [4] logits ready
+  uint64_t* l_full = s_full + 4;              // [4] lse staged
+  uint64_t* item_empty = l_full + 4;          // [4] buffer and lse slot have been read
+  uint64_t* work_full = item_empty + 4;       // [2]
+  uint64_t* work_empty = work_full + 2;       // [2]
+  uint64_t* part_full = work_empty + 2;       // the second warpgroup's sums are there / have been read
+  uint64_t* part_empty = part_full + 1;
+  uint64_t* drain = part_empty + 1;
+  __shared__ PwWork works[2];
+  __shared__ int s_abort;
+  __shared__ uint32_t tmem_slot;
+  volatile int* abort_flag = &s_abort;
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    for (uint32_t i = 0; i < kStages; ++i) { tc_mbar_init(&q_full[i], 1u); tc_mbar_init(&q_empty[i], 1u); }
+    for (int i = 0; i < 2; ++i) {
+      tc_mbar_init(&k_full[i], 1u);
+      tc_mbar_init(&k_empty[i], 1u);
+      tc_mbar_init(&work_full[i], 1u);
+      tc_mbar_init(&work_empty[i], 10u);
+    }
+    for (int i = 0; i < 4; ++i) { tc_mbar_init(&s_full[i], 1u); tc_mbar_init(&l_full[i], 1u); tc_mbar_init(&item_empty[i], 4u); }
+    tc_mbar_init(part_full, 4u);
+    tc_mbar_init(part_empty, 4u);
+    tc_mbar_init(drain, 1u);
+    s_abort = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (warp == 9) { __syncwarp(); tc_alloc(&tmem_slot, 512); }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_slot, 0);
+
+  uint32_t q_issued = 0, k_issued = 0;        // producer: loads issued
+  auto give_up = [&]() { if (!*abort_flag) { if (p.err != nullptr) set_error(p.err, ERRW_TIMEOUT); *abort_flag = 1; } };
+  auto next_work = [&](uint32_t it, PwWork& w) {
+    if (!tc_mbar_poll_warp(&work_full[it & 1], (it >> 1) & 1u, abort_flag)) return false;
+    w = works[it & 1];
+    __syncwarp();
+    if (lane == 0) tc_mbar_arrive(&work_empty[it & 1]);
+    return true;
+  };
+
+  if (warp == 8) {
+    // ---------------- producer ----------------
+    bool ok = true;
+    PwWork w{};
+    auto look_up = [&](uint32_t it) {
+      const long long i = (long long)it * gridDim.x + ((it & 1) ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
+      PackedTile t{};
+      w.found = i / p.Hk < 0x7fffffff && find_packed_tile<kPtTile>(p.seq_start, p.S, p.total, int(i / p.Hk), it == 0 ? p.err : nullptr, t);
+      w.start = t.start; w.len = t.len; w.g = int(i % p.Hk);
+      w.blocks = (t.len + kPtTile - 1) / kPtTile;
+      w.kb = w.blocks - 1 - t.index;          // early keys are seen by most queries: they come first
+      w.qb = max(w.kb, (window > 0 ? max(0, t.len - window) : 0) / kPtTile);
+      if (it >= 2 && !tc_mbar_poll_warp(&work_empty[it & 1], ((it >> 1) - 1) & 1u, abort_flag)) return false;
+      if (lane == 0) { works[it & 1] = w; tc_mbar_arrive(&work_full[it & 1]); }
+      __syncwarp();
+      return true;
+    };
+    ok = look_up(0);
+    for (uint32_t it = 0; ok && w.found; ++it) {
+      const PwWork cur = w;
+      const uint32_t kt = k_issued & 1u;
+      if (k_issued >= 2 && !tc_mbar_poll_warp(&k_empty[kt], ((k_issued >> 1) - 1) & 1u, abort_flag)) { ok = false; break; }
+      if (lane == 0) pt_load_tile<DH>(k_tiles + kt * S::kTileBytes, &maps.k, cur.g, cur.start + cur.kb * kPtTile, &k_full[kt]);
+      ++k_issued;
+      const int per_head = cur.blocks - cur.qb, items = per_head * p.group;
+      int h = cur.g * p.group, qb = cur.qb;
+      for (int i = 0; i < items; ++i) {
+        const uint32_t stage = q_issued % kStages, use = q_issued / kStages;
+        if (use > 0 && !tc_mbar_poll_warp(&q_empty[stage], (use - 1) & 1u, abort_flag)) { ok = false; break; }
+        if (lane == 0) pt_load_tile<DH>(ring + size_t(stage) * S::kTileBytes, &maps.q, h, cur.start + qb * kPtTile, &q_full[stage]);
+        ++q_issued;
+        __syncwarp();
+        if (++qb == cur.blocks) { qb = cur.qb; ++h; }
+        if (i == min(items, int(kStages)) - 1 && !look_up(it + 1)) { ok = false; break; }
+      }
+    }
+    if (!ok && lane == 0) give_up();
+  } else if (warp == 9) {
+    // ---------------- MMA issuer ----------------
+    constexpr uint32_t idesc = tc_idesc(kPtTile, kPtTile);
+    bool ok = true;
+    uint32_t item = 0;
+    for (uint32_t it = 0; ok; ++it) {
+      PwWork w;
+      if (!next_work(it, w)) { ok = false; break; }
+      if (!w.found) break;
+      const int items = __shfl_sync(0xffffffffu, (w.blocks - w.qb) * p.group, 0);
+      const uint32_t kt = it & 1u;
+      if (!tc_mbar_poll_warp(&k_full[kt], (it >> 1) & 1u, abort_flag)) { ok = false; break; }
+      for (int i = 0; i < items; ++i, ++item) {
+        const uint32_t stage = item % kStages, b = item & 3u;
+        if (!tc_mbar_poll_warp(&q_full[stage], (item / kStages) & 1u, abort_flag)) { ok = false; break; }
+        if (item >= 4 && !tc_mbar_poll_warp(&item_empty[b], ((item >> 2) - 1) & 1u, abort_flag)) { ok = false; break; }
+        tc_fence_after();
+        const uint64_t kd = tc_smem_desc(k_tiles + kt * S::kTileBytes), qd = tc_smem_desc(ring + size_t(stage) * S::kTileBytes);
+#pragma unroll
+        for (int k = 0; k < DH / 16; ++k) {
+          const uint64_t at = uint64_t((k / 4) * (kPtTile * 128 / 16) + (k % 4) * 2);
+          tc_mma_bf16_warp(tmem + 128 * b, kd + at, qd + at, idesc, k != 0 ? 1u : 0u);
+        }
+        tc_commit_warp(&s_full[b]);
+        tc_commit_warp(&q_empty[stage]);
+      }
+      if (ok) tc_commit_warp(&k_empty[kt]);
+    }
+    if (!ok) {
+      if (lane == 0) give_up();
+      __syncwarp();
+      tc_commit_warp(drain);
+      int never = 0;
+      tc_mbar_poll_warp(drain, 0u, &never);
+    }
+  } else if (warp == 10) {
+    // ---------------- lse of every item's queries ----------------
+    bool ok = true;
+    uint32_t item = 0;
+    for (uint32_t it = 0; ok; ++it) {
+      PwWork w;
+      if (!next_work(it, w)) { ok = false; break; }
+      if (!w.found) break;
+      for (int h = w.g * p.group; h < (w.g + 1) * p.group && ok; ++h)
+        for (int qb = w.qb; qb < w.blocks; ++qb, ++item) {
+          const uint32_t b = item & 3u;
+          float x[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int i = qb * kPtTile + 32 * e + lane;
+            x[e] = i < w.len ? -1.4426950408889634f * __ldg(lse + size_t(h) * p.total + w.start + i) : 0.f;
+          }
+          if (item >= 4 && !tc_mbar_poll_warp(&item_empty[b], ((item >> 2) - 1) & 1u, abort_flag)) { ok = false; break; }
+#pragma unroll
+          for (int e = 0; e < 4; ++e) offs[b * kPtTile + 32 * e + lane] = x[e];
+          __syncwarp();
+          if (lane == 0) tc_mbar_arrive(&l_full[b]);
+        }
+    }
+    if (!ok && lane == 0) give_up();
+  } else {
+    // ---------------- weights and sums: warpgroup `group_no` takes every second item, one key per thread ----------------
+    const int group_no = warp >> 2, r = threadIdx.x & 127;
+    const uint32_t lanes = uint32_t((warp & 3) * 32) << 16;
+    const float c = p.scale * 1.4426950408889634f;
+    bool ok = true;
+    uint32_t item = 0;
+    for (uint32_t it = 0; ok; ++it) {
+      PwWork w;
+      if (!next_work(it, w)) { ok = false; break; }
+      if (!w.found) break;
+      const int per_head = w.blocks - w.qb, items = per_head * p.group;
+      const int first = window > 0 ? max(0, w.len - window) : 0;
+      const bool last_partial = w.len % kPtTile != 0;
+      double sum = 0.0;
+      int qb = w.qb;
+      for (int i = 0; i < items; ++i, ++item) {
+        const int q0 = qb * kPtTile;
+        const bool masked = qb == w.kb || q0 < first || (last_partial && qb == w.blocks - 1);
+        if (++qb == w.blocks) qb = w.qb;
+        if (int(item & 1u) != group_no) continue;
+        const uint32_t b = item & 3u, s_at = tmem + lanes + 128 * b;
+        const float* off = offs + b * kPtTile;
+        if (!tc_mbar_poll_warp(&l_full[b], (item >> 2) & 1u, abort_flag) || !tc_mbar_poll_warp(&s_full[b], (item >> 2) & 1u, abort_flag)) {
+          ok = false;
+          break;
+        }
+        tc_fence_after();
+        const int lo = max(q0 == w.kb * kPtTile ? r : 0, first - q0), hi = w.len - q0;
+        float part[4];
+        uint32_t s[2][32];
+        __syncwarp();
+        tc_ld_32x32_start(s_at, s[0]);
+        tc_ld_wait(s[0]);
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          if (x < 3) tc_ld_32x32_start(s_at + 32 * (x + 1), s[(x + 1) & 1]);
+          part[x] = masked ? pw_sum32<true>(s[x & 1], off + 32 * x, c, 32 * x, lo, hi) : pw_sum32<false>(s[x & 1], off + 32 * x, c, 0, 0, 0);
+          if (x < 3) tc_ld_wait(s[(x + 1) & 1]);
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) tc_mbar_arrive(&item_empty[b]);
+        sum += double((part[0] + part[1]) + (part[2] + part[3]));
+      }
+      if (!ok) break;
+      // the second warpgroup hands its sums over
+      if (group_no == 1) {
+        if (it > 0 && !tc_mbar_poll_warp(part_empty, (it - 1) & 1u, abort_flag)) { ok = false; break; }
+        partial[r] = sum;
+        __syncwarp();
+        if (lane == 0) tc_mbar_arrive(part_full);
+      } else {
+        if (!tc_mbar_poll_warp(part_full, it & 1u, abort_flag)) { ok = false; break; }
+        const float total = float(sum + partial[r]);
+        __syncwarp();
+        if (lane == 0) tc_mbar_arrive(part_empty);
+        if (w.kb * kPtTile + r < w.len) acc[size_t(w.g) * p.total + w.start + w.kb * kPtTile + r] = total;
+      }
+    }
+    if (!ok && lane == 0) give_up();
+  }
+
+  tc_fence_before();
+  __syncthreads();
+  if (*abort_flag) {                          // copies in flight have to land before the CTA ends
+    if (warp == 8) {
+      int never = 0;
+      for (uint32_t i = q_issued > kStages ? q_issued - kStages : 0u; i < q_issued; ++i) tc_mbar_poll(&q_full[i % kStages], (i / kStages) & 1u, &never);
+      for (uint32_t i = k_issued > 2 ? k_issued - 2 : 0u; i < k_issued; ++i) tc_mbar_poll(&k_full[i & 1u], (i >> 1) & 1u, &never);
+    }
+    __syncthreads();
+  }
+  tc_fence_after();
+  if (warp == 9) { __syncwarp(); tc_dealloc(tmem, 512); }
+}
+
+}  // namespace adore

@@ -49,9 +49,19 @@ __device__ __forceinline__ bool tc_mbar_wait(uint64_t* bar, uint32_t parity, vol
   }
   return true;
 }
+// The same without a look at the clock on the way: a handful of cycles less per hand-over. It gives up after kTcWaitPolls polls,
+// each of which may itself sleep for a while in hardware.
+constexpr uint32_t kTcWaitPolls = 1u << 22;
+__device__ __forceinline__ bool tc_mbar_poll(uint64_t* bar, uint32_t parity, volatile int* abort) {
+  for (uint32_t i = 0; i < kTcWaitPolls; ++i) {
+    if (tc_mbar_try(bar, parity)) return true;
+    if ((i & 63u) == 63u && *abort) return false;
+  }
+  return false;
+}
 // The same for a whole warp, with one answer for all its lanes (the warp goes on to warp-collective instructions).
-__device__ __forceinline__ bool tc_mbar_wait_warp(uint64_t* bar, uint32_t parity, volatile int* abort) {
-  return __all_sync(0xffffffffu, tc_mbar_wait(bar, parity, abort));
+__device__ __forceinline__ bool tc_mbar_poll_warp(uint64_t* bar, uint32_t parity, volatile int* abort) {
+  return __all_sync(0xffffffffu, tc_mbar_poll(bar, parity, abort));
 }
 __device__ __forceinline__ void tc_tma_load_2d(void* dst, const CUtensorMap* map, int x, int y, uint64_t* bar) {
   asm volatile(
@@ -136,13 +146,33 @@ __device__ __forceinline__ void tc_st_32x32(uint32_t taddr, const uint32_t (&r)[
       "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(taddr) : "memory");
 }
 __device__ __forceinline__ void tc_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-// D[tmem] (+)= A[tmem] * B[smem], bf16 inputs, fp32 accumulate, M = 128
-__device__ __forceinline__ void tc_mma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+// Products and commits that a whole converged warp calls, with the same operands in all lanes, and one elected lane issues. (An
+// MMA takes its operands from uniform registers: inside a branch of one lane each of them is moved there on its own, which cost
+// about 80 cycles per MMA.)
+// D[tmem] (+)= A[smem] * B[smem]^T, bf16 inputs, fp32 accumulate, M = 128
+__device__ __forceinline__ void tc_mma_bf16_warp(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\t"
+      "{\n\t.reg .pred p, e;\n\t"
       "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+      "elect.sync _|e, 0xffffffff;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+      ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
+}
+// The same with A in TMEM.
+__device__ __forceinline__ void tc_mma_bf16_ts_warp(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p, e;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "elect.sync _|e, 0xffffffff;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
       ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void tc_commit_warp(uint64_t* bar) {
+  asm volatile(
+      "{\n\t.reg .pred e;\n\t"
+      "elect.sync _|e, 0xffffffff;\n\t"
+      "@e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}"
+      ::"r"(tc_smem_u32(bar)) : "memory");
 }
 __device__ __forceinline__ void tc_tma_load_3d(void* dst, const CUtensorMap* map, int x, int y, int z, uint64_t* bar) {
   asm volatile(

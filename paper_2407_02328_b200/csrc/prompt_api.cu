@@ -208,13 +208,47 @@ adore_status_t step_rows(const adore_q4_t* c, const float* weights, const void* 
   return launched();
 }
 
+// CTAs that share a (sequence, key/value head, head block): the count n of 1..16 whose waves of CTAs (two on an SM) times a
+// CTA's chunks per warp is smallest, with two chunks' time added for a CTA's start and the joins.
+int q4_split(int64_t units, int chunks, int sms) {
+  int best = 1;
+  int64_t least = INT64_MAX;
+  for (int n = 1; n <= 16; ++n) {
+    const int64_t waves = (units * n + 2 * sms - 1) / (2 * sms), each = (chunks + kQ4Warps * n - 1) / (kQ4Warps * n);
+    const int64_t cost = waves * (each + 2);
+    if (cost < least) { least = cost; best = n; }
+  }
+  return best;
+}
+
+template <typename T, int DH, int HB>
+adore_status_t attend_q4_as(const adore_q4_t* c, const void* q, const void* k, const void* v, const Q4Rows& rows, const int* slot_pos, void* out,
+                            float* weights, cudaStream_t st) {
+  auto kernel = q4_attention_kernel<T, DH, HB>;
+  constexpr size_t smem = q4_attention_smem<T, DH, HB>();
+  const int P = q4_padded(c->capacity), blocks = (c->n_heads / c->n_kv_heads + HB - 1) / HB;
+  const int64_t units = int64_t(c->batch) * c->n_kv_heads * blocks;
+  const int ctas = q4_split(units, P / kQ4Chunk, sm_count());
+  if (units * ctas > kMaxGrid) return ADORE_ERR_UNSUPPORTED;
+  if (!allow_smem(kernel, smem)) return ADORE_ERR_CUDA;
+  if (ctas > 8 && cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) { cudaGetLastError(); return ADORE_ERR_CUDA; }
+  cudaLaunchConfig_t lc{};
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim.x = unsigned(ctas); at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
+  lc.gridDim = dim3(unsigned(units * ctas)); lc.blockDim = dim3(kQ4Threads); lc.dynamicSmemBytes = smem; lc.stream = st;
+  lc.attrs = at; lc.numAttrs = ctas > 1 ? 1 : 0;
+  const cudaError_t e = cudaLaunchKernelEx(&lc, kernel, rows, c->n_heads, c->n_kv_heads, c->capacity, P, blocks, ctas, scale_of(c->scale, DH),
+                                           static_cast<const T*>(q), static_cast<const T*>(k), static_cast<const T*>(v), slot_pos,
+                                           static_cast<T*>(out), weights);
+  if (e != cudaSuccess) { cudaGetLastError(); return ADORE_ERR_CUDA; }
+  return launched();
+}
 template <typename T, int DH>
 adore_status_t attend_q4(const adore_q4_t* c, const void* q, const void* k, const void* v, const Q4Rows& rows, const int* slot_pos, void* out,
                          float* weights, cudaStream_t st) {
-  q4_attention_simple_kernel<T, DH><<<unsigned(c->batch * c->n_heads), 32, 0, st>>>(
-      rows, c->n_heads, c->n_kv_heads, c->capacity, q4_padded(c->capacity), scale_of(c->scale, DH), static_cast<const T*>(q),
-      static_cast<const T*>(k), static_cast<const T*>(v), slot_pos, static_cast<T*>(out), weights);
-  return launched();
+  return c->n_heads / c->n_kv_heads <= 8 ? attend_q4_as<T, DH, 8>(c, q, k, v, rows, slot_pos, out, weights, st)
+                                         : attend_q4_as<T, DH, 16>(c, q, k, v, rows, slot_pos, out, weights, st);
 }
 
 template <typename T, int DH>

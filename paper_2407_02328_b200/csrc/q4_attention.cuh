@@ -1,67 +1,476 @@
-// Decode attention over 4-bit rows: one warp per (sequence, query head), the head dimension spread over the lanes, one slot
-// at a time with a running maximum and sum.
+// Decode attention over 4-bit rows.
+//
+//   x_s = scale q . (code_s step_s + low_s) = scale sum_groups (step_s sum code q + low_s sum q)      (s: slots; groups of 64)
+//   out = sum_s softmax(x)_s (code_s step_s + low_s)
+//
+// Bound by reading the rows: 144 bytes per slot and key/value head at dh = 128 (72 at 64). The codes go into the matrix
+// instructions as they are, so that no element is ever expanded to a full value: with B = codes of 8 slots x 16 elements
+// and A = up to 16 query heads, one mma.m16n8k16 gives 128 partial logits; step and low are applied per slot and group to its
+// result. Query heads of a key/value head share the rows; with 8 or fewer heads half of the instruction's rows stay empty,
+// which costs nothing that bounds the kernel (legacy mma.sync: 64 of them per 16 slots and SM are far below its rate).
+//   logits: A = q as bfloat16 terms (one if T is bfloat16, exact; three if float, 24 bits), scaled by a power of two per head.
+//           B = the code's 4 bits as the lowest bits of a bfloat16, a subnormal number code 2^-133: one AND per two codes.
+//   values: A = weight x step of the slot as bfloat16 (T bfloat16: rounded, half a step 2^-8, as the output is; float: three
+//           terms), B = the codes as bfloat16 numbers (128 + code by an OR, minus 128).
+// A CTA is 8 warps, each with its own chunks of 16 slots, its own ring of shared-memory stages (cp.async, no barrier between
+// warps), running maximum, sum and accumulators. Warps are joined through shared memory, the CTAs that share a (sequence,
+// key/value head, block of 16 query heads) through a cluster's distributed shared memory: one launch, no workspace. The
+// maximum that the weights refer to is only raised when it grew by more than 2^8, so the accumulators are hardly ever rescaled.
+// Per-slot weights: the logits go to the weights' own places first and are turned into weights by the lanes that wrote them.
 #pragma once
+
+#include <cooperative_groups.h>
 
 #include "q4.cuh"
 
 namespace adore {
 
-template <typename T, int DH>
-__global__ void __launch_bounds__(32) q4_attention_simple_kernel(const Q4Rows c, int H, int Hk, int C, int P, float scale, const T* q,
-                                                                 const T* k_new, const T* v_new, const int* slot_pos, T* out,
-                                                                 float* weights) {
-  const int bh = blockIdx.x, b = bh / H, g = (bh % H) / (H / Hk), lane = threadIdx.x;
-  const size_t r = size_t(b) * Hk + g;
-  constexpr int LPR = DH / 8;
-  const int j = lane % LPR;
-  const bool on = lane < LPR;
-  float qx[8], o[8];
-  load8(q + size_t(bh) * DH + 8 * j, qx);
-  for (int e = 0; e < 8; ++e) o[e] = 0.f;
-  float m = -INFINITY, l = 0.f;
-  float* w = weights != nullptr ? weights + size_t(bh) * (size_t(C) + 1) : nullptr;
-  for (int s = 0; s <= C; ++s) {
-    float kx[8], vx[8];
-    bool have;
-    if (s < C) {
-      have = slot_pos[r * C + s] >= 0;
-      if (have) {
-        const uint32_t kw = c.k[(r * P + s) * (DH / 8) + q4_k_word<DH>(j)];
-        const uint32_t* vp = c.v + (r * (P / 2) + s / 2) * (DH / 4) + q4_v_word<DH>(j);
-        const int sh = (s & 1) * 16;
-        const uint32_t vw = ((vp[0] >> sh) & 0xffffu) | ((vp[DH / 32] >> sh) << 16);
-        const float2 ks = __bfloat1622float2(c.kp[(r * P + s) * (DH / kQ4Group) + (j >> 3)]);
-        const float2 vs = __bfloat1622float2(c.vp[(r * P + s) * (DH / kQ4Group) + (j >> 3)]);
-        for (int e = 0; e < 8; ++e) {
-          kx[e] = fmaf(float((kw >> (4 * e)) & 15u), ks.x, ks.y);
-          vx[e] = fmaf(float((vw >> (4 * e)) & 15u), vs.x, vs.y);
+constexpr int kQ4Warps = 8;
+constexpr int kQ4Threads = 32 * kQ4Warps;
+constexpr int kQ4Chunk = 16;                // slots a warp takes at a time
+constexpr int kQ4Stages = 4;
+constexpr float kQ4Nothing = -1e30f;        // running maximum before any slot; finite, so that differences are never NaN
+
+template <int DH>
+struct Q4Smem {
+  static constexpr int kCodeBytes = kQ4Chunk * DH / 2;
+  static constexpr int kPairBytes = kQ4Chunk * (DH / kQ4Group) * 4;
+  static constexpr int kStageBytes = 2 * kCodeBytes + 2 * kPairBytes;
+  static constexpr int kRing = kQ4Warps * kQ4Stages * kStageBytes;
+};
+template <typename T, int DH, int HB>
+__host__ __device__ constexpr size_t q4_attention_smem() {
+  // the ring, later the warps' accumulators; the query fragments of float heads
+  const size_t ring = Q4Smem<DH>::kRing, acc = size_t(kQ4Warps) * HB * DH * 4;
+  return (ring > acc ? ring : acc) + (sizeof(T) == 4 ? size_t(DH / 16) * 3 * 32 * 16 : 0);
+}
+
+__device__ __forceinline__ void q4_copy16(void* dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(static_cast<uint32_t>(__cvta_generic_to_shared(dst))), "l"(src) : "memory");
+}
+__device__ __forceinline__ void q4_mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t q4_bf16x2(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+__device__ __forceinline__ float q4_low_half(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float q4_high_half(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
+// The first `TERMS` bfloat16 terms of two values (v = t0 + t1 + t2 + ..).
+template <int TERMS>
+__device__ __forceinline__ void q4_terms(float a, float b, uint32_t (&t)[TERMS]) {
+#pragma unroll
+  for (int i = 0; i < TERMS; ++i) {
+    t[i] = q4_bf16x2(a, b);
+    a -= q4_low_half(t[i]);
+    b -= q4_high_half(t[i]);
+  }
+}
+__device__ __forceinline__ float q4_exp2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// Codes of four pairs of elements as bfloat16 pairs: subnormal (code 2^-133), or the numbers themselves.
+__device__ __forceinline__ uint32_t q4_tiny(uint32_t w, int n) { return (w >> (4 * n)) & 0x000f000fu; }
+__device__ __forceinline__ uint32_t q4_number(uint32_t w, int n) {
+  uint32_t r;
+  const uint32_t x = ((w >> (4 * n)) & 0x000f000fu) | 0x43004300u;      // 128 + code
+  asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(x), "r"(0x43004300u));
+  return r;
+}
+
+// Words of one lane's piece.
+template <int N>
+__device__ __forceinline__ void q4_lds(const void* p, uint32_t (&w)[N]) {
+  if constexpr (N == 4) {
+    const uint4 x = *static_cast<const uint4*>(p);
+    w[0] = x.x; w[1] = x.y; w[2] = x.z; w[3] = x.w;
+  } else {
+    const uint2 x = *static_cast<const uint2*>(p);
+    w[0] = x.x; w[1] = x.y;
+  }
+}
+
+// HB: query heads of a block, 8 or 16 (8: rows 8..15 of the matrix instructions are empty).
+template <typename T, int DH, int HB>
+__global__ void __launch_bounds__(kQ4Threads, 2)
+q4_attention_kernel(const Q4Rows c, int H, int Hk, int C, int P, int blocks, int ctas, float scale, const T* q, const T* k_new, const T* v_new,
+                    const int* slot_pos, T* out, float* weights) {
+  using S = Q4Smem<DH>;
+  constexpr int TERMS = sizeof(T) == 4 ? 3 : 1;
+  constexpr int NW = DH / 32;                 // words of a lane's piece of a row
+  constexpr int NG = DH / kQ4Group;
+  constexpr int NR = HB / 8;                  // accumulator rows of a lane that hold heads
+  extern __shared__ __align__(16) unsigned char q4_smem[];
+  uint4* q_frag = reinterpret_cast<uint4*>(q4_smem + (q4_attention_smem<T, DH, HB>() - (TERMS == 3 ? size_t(DH / 16) * 3 * 32 * 16 : 0)));
+  __shared__ float s_m[kQ4Warps][HB], s_l[kQ4Warps][HB], s_low[kQ4Warps][HB][NG];
+  __shared__ float s_new[HB];                 // logits of the token's own row (log 2 units)
+  __shared__ float s_cta_m[HB], s_cta_l[HB];  // this CTA's, read by the cluster
+  __shared__ float s_scale[16][HB];           // factor of every CTA of the cluster in the result
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gid = lane >> 2, tig = lane & 3;
+  const int rank = blockIdx.x % ctas, unit = blockIdx.x / ctas;
+  const int hb = unit % blocks;
+  const size_t r = unit / blocks;             // sequence x key/value head
+  const int b = int(r / Hk), g = int(r % Hk), group = H / Hk;
+  const int nh = min(HB, group - hb * HB);    // heads of this block
+  const size_t h0 = size_t(b) * H + size_t(g) * group + hb * HB;
+  const float to_log2 = scale * 1.4426950408889634f;
+
+  // ---- loads of a chunk into a stage of this warp's ring
+  const int chunks = P / kQ4Chunk, step = ctas * kQ4Warps;
+  unsigned char* ring = q4_smem + warp * (kQ4Stages * S::kStageBytes);
+  auto load = [&](int chunk, int stage) {
+    if (chunk < chunks) {
+      unsigned char* d = ring + stage * S::kStageBytes;
+      const size_t at = r * P + size_t(chunk) * kQ4Chunk;
+      const unsigned char* ks = reinterpret_cast<const unsigned char*>(c.k) + at * (DH / 2);
+      const unsigned char* vs = reinterpret_cast<const unsigned char*>(c.v) + at * (DH / 2);
+#pragma unroll
+      for (int i = 0; i < S::kCodeBytes / 512; ++i) {
+        q4_copy16(d + 512 * i + 16 * lane, ks + 512 * i + 16 * lane);
+        q4_copy16(d + S::kCodeBytes + 512 * i + 16 * lane, vs + 512 * i + 16 * lane);
+      }
+      constexpr int kPieces = S::kPairBytes / 16;
+      if (lane < 2 * kPieces) {
+        const int i = lane % kPieces;
+        const unsigned char* src = reinterpret_cast<const unsigned char*>(lane < kPieces ? c.kp : c.vp) + at * (NG * 4) + 16 * i;
+        q4_copy16(d + 2 * S::kCodeBytes + 16 * lane, src);
+      }
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  const int first = rank * kQ4Warps + warp;
+#pragma unroll
+  for (int i = 0; i < kQ4Stages - 1; ++i) load(first + i * step, i);
+
+  // ---- queries: bfloat16 fragments, the sums that the low values meet
+  uint32_t qa[TERMS == 1 ? DH / 16 : 1][4];
+  float qsum[NR][NG], unit_x[NR];
+  float qx[NR][NW][8];
+#pragma unroll
+  for (int y = 0; y < NR; ++y) {
+    const bool have = gid + 8 * y < nh;
+    float top = 0.f;
+#pragma unroll
+    for (int n = 0; n < NG; ++n) qsum[y][n] = 0.f;
+#pragma unroll
+    for (int i = 0; i < NW; ++i) {
+      if (have) load8(q + (h0 + gid + 8 * y) * DH + 32 * i + 8 * tig, qx[y][i]);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        if (!have) qx[y][i][e] = 0.f;
+        top = fmaxf(top, fabsf(qx[y][i][e]));
+        qsum[y][i / 2] += qx[y][i][e];
+      }
+    }
+#pragma unroll
+    for (int o = 1; o < 4; o <<= 1) {
+      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+#pragma unroll
+      for (int n = 0; n < NG; ++n) qsum[y][n] += __shfl_xor_sync(0xffffffffu, qsum[y][n], o);
+    }
+    // largest element to [1, 2) 2^126; a code is 2^-133, so a product is 2^-7 of the plain one
+    const int e2 = max(-120, min(120, (int(__float_as_uint(top) >> 23) & 255) - 127));
+    const float to_unit = __uint_as_float(uint32_t(127 - e2) << 23);
+#pragma unroll
+    for (int i = 0; i < NW; ++i)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) qx[y][i][e] = qx[y][i][e] * to_unit * 8.507059173023462e37f;      // 2^126
+    unit_x[y] = to_log2 * 128.f * __uint_as_float(uint32_t(127 + e2) << 23);
+#pragma unroll
+    for (int n = 0; n < NG; ++n) qsum[y][n] *= to_log2;
+  }
+#pragma unroll
+  for (int i = 0; i < NW; ++i)
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+      // step 2 i + m: k = 2 tig, 2 tig + 1 are elements 2 m, 2 m + 4 of the lane's 8; k + 8 the ones behind them
+      uint32_t t0[TERMS], t1[TERMS] = {}, t2[TERMS], t3[TERMS] = {};
+      q4_terms<TERMS>(qx[0][i][2 * m], qx[0][i][2 * m + 4], t0);
+      q4_terms<TERMS>(qx[0][i][2 * m + 1], qx[0][i][2 * m + 5], t2);
+      if (NR == 2) {
+        q4_terms<TERMS>(qx[NR - 1][i][2 * m], qx[NR - 1][i][2 * m + 4], t1);
+        q4_terms<TERMS>(qx[NR - 1][i][2 * m + 1], qx[NR - 1][i][2 * m + 5], t3);
+      }
+      if constexpr (TERMS == 1) {
+        qa[2 * i + m][0] = t0[0]; qa[2 * i + m][1] = t1[0]; qa[2 * i + m][2] = t2[0]; qa[2 * i + m][3] = t3[0];
+      } else if (warp == 0) {
+#pragma unroll
+        for (int x = 0; x < TERMS; ++x) q_frag[((2 * i + m) * TERMS + x) * 32 + lane] = make_uint4(t0[x], t1[x], t2[x], t3[x]);
+      }
+    }
+  if constexpr (TERMS == 3) __syncthreads();
+
+  // ---- the token's own row: one warp per head
+  if (rank == 0)
+    for (int h = warp; h < HB; h += kQ4Warps) {
+      float x = 0.f;
+      if (k_new != nullptr && h < nh)
+        for (int e = lane; e < DH; e += 32) x = fmaf(Elem<T>::to_float(q[(h0 + h) * DH + e]), Elem<T>::to_float(k_new[r * DH + e]), x);
+      x = warp_sum(x);
+      if (lane == 0) s_new[h] = k_new != nullptr ? x * to_log2 : kQ4Nothing;
+    }
+
+  // ---- this warp's chunks
+  float o[DH / 8][4];
+  float m[NR], l[NR], low_acc[NR][NG];
+#pragma unroll
+  for (int i = 0; i < DH / 8; ++i)
+#pragma unroll
+    for (int x = 0; x < 4; ++x) o[i][x] = 0.f;
+#pragma unroll
+  for (int y = 0; y < NR; ++y) {
+    m[y] = kQ4Nothing;
+    l[y] = 0.f;
+#pragma unroll
+    for (int n = 0; n < NG; ++n) low_acc[y][n] = 0.f;
+  }
+  const int* pos = slot_pos + r * C;
+  auto occupied = [&](int chunk, bool (&have)[2][2]) {
+#pragma unroll
+    for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const int s = chunk * kQ4Chunk + 8 * nt + 2 * tig + x;
+        have[nt][x] = chunk < chunks && s < C && __ldg(pos + s) >= 0;
+      }
+  };
+  bool have[2][2], have_next[2][2];
+  occupied(first, have);
+  int stage = 0;
+  for (int chunk = first; chunk < chunks; chunk += step) {
+    load(chunk + (kQ4Stages - 1) * step, (stage + kQ4Stages - 1) % kQ4Stages);
+    occupied(chunk + step, have_next);
+    asm volatile("cp.async.wait_group %0;" ::"n"(kQ4Stages - 1) : "memory");
+    __syncwarp();
+    const unsigned char* d = ring + stage * S::kStageBytes;
+    // logits of 2 x 8 slots: this lane's are slots 2 tig, 2 tig + 1 of heads gid (and gid + 8)
+    float x[2][NR][2];
+#pragma unroll
+    for (int nt = 0; nt < 2; ++nt) {
+      uint32_t w[NW], pair[2 * NG];
+      q4_lds<NW>(d + (8 * nt + gid) * (DH / 2) + tig * (4 * NW), w);
+      q4_lds<2 * NG>(d + 2 * S::kCodeBytes + (8 * nt + 2 * tig) * (NG * 4), pair);
+#pragma unroll
+      for (int y = 0; y < NR; ++y) x[nt][y][0] = x[nt][y][1] = 0.f;
+#pragma unroll
+      for (int n = 0; n < NG; ++n) {
+        float acc[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 2 * n; i < 2 * n + 2; ++i)
+#pragma unroll
+          for (int mm = 0; mm < 2; ++mm) {
+            const uint32_t b0 = q4_tiny(w[i], 2 * mm), b1 = q4_tiny(w[i], 2 * mm + 1);
+            if constexpr (TERMS == 1) {
+              q4_mma(acc, qa[2 * i + mm], b0, b1);
+            } else {
+#pragma unroll
+              for (int t = TERMS - 1; t >= 0; --t) {
+                const uint4 f = q_frag[((2 * i + mm) * TERMS + t) * 32 + lane];
+                const uint32_t a[4] = {f.x, f.y, f.z, f.w};
+                q4_mma(acc, a, b0, b1);
+              }
+            }
+          }
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const float st = q4_low_half(pair[e * NG + n]), lo = q4_high_half(pair[e * NG + n]);
+#pragma unroll
+          for (int y = 0; y < NR; ++y) x[nt][y][e] = fmaf(acc[2 * y + e] * unit_x[y], st, fmaf(lo, qsum[y][n], x[nt][y][e]));
         }
       }
-    } else {
-      have = k_new != nullptr;
-      if (have) {
-        load8(k_new + r * DH + 8 * j, kx);
-        load8(v_new + r * DH + 8 * j, vx);
+    }
+    float top[NR];
+    bool raise = false;
+#pragma unroll
+    for (int y = 0; y < NR; ++y) {
+#pragma unroll
+      for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+          if (!have[nt][e]) x[nt][y][e] = -INFINITY;
+      top[y] = fmaxf(fmaxf(x[0][y][0], x[0][y][1]), fmaxf(x[1][y][0], x[1][y][1]));
+      raise |= top[y] - m[y] > 8.f;
+    }
+    if (__any_sync(0xffffffffu, raise)) {
+#pragma unroll
+      for (int y = 0; y < NR; ++y) {
+#pragma unroll
+        for (int w = 1; w < 4; w <<= 1) top[y] = fmaxf(top[y], __shfl_xor_sync(0xffffffffu, top[y], w));
+        const float now = fmaxf(m[y], top[y]), f = q4_exp2(m[y] - now);
+        m[y] = now;
+        l[y] *= f;
+#pragma unroll
+        for (int n = 0; n < NG; ++n) low_acc[y][n] *= f;
+#pragma unroll
+        for (int i = 0; i < DH / 8; ++i) { o[i][2 * y] *= f; o[i][2 * y + 1] *= f; }
       }
     }
-    float x = -INFINITY;
-    if (have) {
-      float d = 0.f;
-      for (int e = 0; e < 8; ++e) d = fmaf(qx[e], kx[e], d);
-      x = warp_sum(on ? d : 0.f) * scale;
-      const float now = fmaxf(m, x), f = expf(m - now), p = expf(x - now);
-      m = now;
-      l = l * f + p;
-      for (int e = 0; e < 8; ++e) o[e] = o[e] * f + p * vx[e];
+    if (weights != nullptr) {
+#pragma unroll
+      for (int y = 0; y < NR; ++y)
+        if (gid + 8 * y < nh) {
+          float* row = weights + (h0 + gid + 8 * y) * (size_t(C) + 1) + chunk * kQ4Chunk;
+#pragma unroll
+          for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+              if (chunk * kQ4Chunk + 8 * nt + 2 * tig + e < C) row[8 * nt + 2 * tig + e] = x[nt][y][e];
+        }
     }
-    if (w != nullptr && lane == 0) w[s] = x;
+#pragma unroll
+    for (int y = 0; y < NR; ++y)
+#pragma unroll
+      for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          x[nt][y][e] = q4_exp2(x[nt][y][e] - m[y]);
+          l[y] += x[nt][y][e];
+        }
+    // values: k = slots 2 tig, 2 tig + 1 (nt = 0) and those + 8 (nt = 1)
+    uint32_t vw[2][NW], pair[2][2 * NG];
+#pragma unroll
+    for (int nt = 0; nt < 2; ++nt) {
+      q4_lds<NW>(d + S::kCodeBytes + (4 * nt + tig) * DH + gid * (4 * NW), vw[nt]);
+      q4_lds<2 * NG>(d + 2 * S::kCodeBytes + S::kPairBytes + (8 * nt + 2 * tig) * (NG * 4), pair[nt]);
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+#pragma unroll
+        for (int n = 0; n < NG; ++n)
+          if (!have[nt][e]) pair[nt][e * NG + n] = 0u;             // an empty slot may hold anything
+    }
+#pragma unroll
+    for (int n = 0; n < NG; ++n) {
+      uint32_t a[TERMS][4];
+#pragma unroll
+      for (int nt = 0; nt < 2; ++nt) {
+        const float s0 = q4_low_half(pair[nt][n]), s1 = q4_low_half(pair[nt][NG + n]);
+        const float l0 = q4_high_half(pair[nt][n]), l1 = q4_high_half(pair[nt][NG + n]);
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+          uint32_t t[TERMS] = {};
+          if (y < NR) {
+            q4_terms<TERMS>(x[nt][y < NR ? y : 0][0] * s0, x[nt][y < NR ? y : 0][1] * s1, t);
+            low_acc[y < NR ? y : 0][n] += fmaf(x[nt][y < NR ? y : 0][0], l0, x[nt][y < NR ? y : 0][1] * l1);
+          }
+#pragma unroll
+          for (int z = 0; z < TERMS; ++z) a[z][2 * nt + y] = t[z];
+        }
+      }
+#pragma unroll
+      for (int i = 2 * n; i < 2 * n + 2; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t b0 = q4_number(vw[0][i], e), b1 = q4_number(vw[1][i], e);
+#pragma unroll
+          for (int z = TERMS - 1; z >= 0; --z) q4_mma(o[4 * i + e], a[z], b0, b1);
+        }
+    }
+#pragma unroll
+    for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) have[nt][e] = have_next[nt][e];
+    stage = stage + 1 == kQ4Stages ? 0 : stage + 1;
+    __syncwarp();                             // the stage has been read before it is filled again
   }
-  const float inv = l > 0.f ? 1.f / l : 0.f;
-  for (int e = 0; e < 8; ++e) o[e] *= inv;
-  if (on) store8(out + size_t(bh) * DH + 8 * j, o);
-  __syncwarp();
-  if (w != nullptr)
-    for (int s = lane; s <= C; s += 32) w[s] = w[s] == -INFINITY ? 0.f : expf(w[s] - m) * inv;
+  asm volatile("cp.async.wait_all;" ::: "memory");
+
+  // ---- join the warps
+#pragma unroll
+  for (int y = 0; y < NR; ++y) {
+#pragma unroll
+    for (int w = 1; w < 4; w <<= 1) {
+      l[y] += __shfl_xor_sync(0xffffffffu, l[y], w);
+#pragma unroll
+      for (int n = 0; n < NG; ++n) low_acc[y][n] += __shfl_xor_sync(0xffffffffu, low_acc[y][n], w);
+    }
+    if (tig == 0) {
+      s_m[warp][gid + 8 * y] = m[y];
+      s_l[warp][gid + 8 * y] = l[y];
+#pragma unroll
+      for (int n = 0; n < NG; ++n) s_low[warp][gid + 8 * y][n] = low_acc[y][n];
+    }
+  }
+  __syncthreads();                            // every warp is done with its ring
+  float* part = reinterpret_cast<float*>(q4_smem);                 // [warp][HB][DH]
+#pragma unroll
+  for (int i = 0; i < DH / 8; ++i)
+#pragma unroll
+    for (int y = 0; y < NR; ++y)
+#pragma unroll
+      for (int e = 0; e < 2; ++e)             // n-tile 4 w + n, column j: element 32 w + 4 j + n
+        part[(warp * HB + gid + 8 * y) * DH + 32 * (i / 4) + 4 * (2 * tig + e) + i % 4] = o[i][2 * y + e];
+  __syncthreads();
+  if (threadIdx.x < HB) {
+    float top = kQ4Nothing, sum = 0.f;
+    for (int w = 0; w < kQ4Warps; ++w) top = fmaxf(top, s_m[w][threadIdx.x]);
+    for (int w = 0; w < kQ4Warps; ++w) sum += s_l[w][threadIdx.x] * q4_exp2(s_m[w][threadIdx.x] - top);
+    s_cta_m[threadIdx.x] = top;
+    s_cta_l[threadIdx.x] = sum;
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < HB * DH; i += kQ4Threads) {
+    const int h = i / DH, e = i % DH;
+    float sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < kQ4Warps; ++w) sum += (part[(w * HB + h) * DH + e] + s_low[w][h][e / kQ4Group]) * q4_exp2(s_m[w][h] - s_cta_m[h]);
+    part[h * DH + e] = sum;                   // (only this thread reads or writes column e of head h)
+  }
+
+  // ---- join the CTAs of the cluster
+  namespace cg = cooperative_groups;
+  cg::cluster_group cluster = cg::this_cluster();
+  if (ctas > 1) cluster.sync();
+  else __syncthreads();
+  __shared__ float s_top[HB], s_inv[HB];
+  if (threadIdx.x < HB) {
+    const int h = threadIdx.x;
+    const float own = ctas > 1 ? *cluster.map_shared_rank(&s_new[h], 0) : s_new[h];
+    float top = own, sum = 0.f;
+    for (int i = 0; i < ctas; ++i) top = fmaxf(top, ctas > 1 ? *cluster.map_shared_rank(&s_cta_m[h], i) : s_cta_m[h]);
+    for (int i = 0; i < ctas; ++i) {
+      const float f = q4_exp2((ctas > 1 ? *cluster.map_shared_rank(&s_cta_m[h], i) : s_cta_m[h]) - top);
+      s_scale[i][h] = f;
+      sum += f * (ctas > 1 ? *cluster.map_shared_rank(&s_cta_l[h], i) : s_cta_l[h]);
+    }
+    const float mine = k_new != nullptr ? q4_exp2(own - top) : 0.f;
+    sum += mine;
+    s_top[h] = top;
+    s_inv[h] = sum > 0.f ? 1.f / sum : 0.f;
+    s_l[0][h] = mine;                         // weight of the token's own row, not yet divided
+  }
+  __syncthreads();
+  for (int i = rank * kQ4Threads + threadIdx.x; i < nh * DH; i += ctas * kQ4Threads) {
+    const int h = i / DH, e = i % DH;
+    float sum = 0.f;
+    for (int x = 0; x < ctas; ++x) sum += (ctas > 1 ? *cluster.map_shared_rank(&part[i], x) : part[i]) * s_scale[x][h];
+    if (v_new != nullptr) sum = fmaf(s_l[0][h], Elem<T>::to_float(v_new[r * DH + e]), sum);
+    out[(h0 + h) * DH + e] = Elem<T>::from_float(sum * s_inv[h]);
+  }
+  if (weights != nullptr) {
+#pragma unroll
+    for (int y = 0; y < NR; ++y) {
+      const int h = gid + 8 * y;
+      if (h >= nh) continue;
+      float* row = weights + (h0 + h) * (size_t(C) + 1);
+      const float top = s_top[h], inv = s_inv[h];
+      for (int chunk = first; chunk < chunks; chunk += step)
+#pragma unroll
+        for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const int s = chunk * kQ4Chunk + 8 * nt + 2 * tig + e;
+            if (s < C) row[s] = q4_exp2(row[s] - top) * inv;
+          }
+      if (rank == 0 && warp == 0 && tig == 0) row[C] = s_l[0][h] * inv;
+    }
+  }
+  if (ctas > 1) cluster.sync();               // nobody leaves while its shared memory is read
 }
 
 }  // namespace adore

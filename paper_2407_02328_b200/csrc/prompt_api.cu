@@ -208,14 +208,15 @@ adore_status_t step_rows(const adore_q4_t* c, const float* weights, const void* 
   return launched();
 }
 
-// CTAs that share a (sequence, key/value head, head block): the count n of 1..16 whose waves of CTAs (two on an SM) times a
-// CTA's chunks per warp is smallest, with two chunks' time added for a CTA's start and the joins.
+// CTAs that share a (sequence, key/value head, head block): the count n of 1..16 with the least time for the fullest SM. A CTA
+// costs its chunks per warp and about three chunks' time for its start and the joins; an SM's CTAs share the bandwidth, but
+// fewer than three cannot use it up.
 int q4_split(int64_t units, int chunks, int sms) {
   int best = 1;
   int64_t least = INT64_MAX;
   for (int n = 1; n <= 16; ++n) {
-    const int64_t waves = (units * n + 2 * sms - 1) / (2 * sms), each = (chunks + kQ4Warps * n - 1) / (kQ4Warps * n);
-    const int64_t cost = waves * (each + 2);
+    const int64_t on_sm = (units * n + sms - 1) / sms, each = (chunks + kQ4Warps * n - 1) / (kQ4Warps * n) + 3;
+    const int64_t cost = std::max<int64_t>(on_sm, 3) * each;
     if (cost < least) { least = cost; best = n; }
   }
   return best;

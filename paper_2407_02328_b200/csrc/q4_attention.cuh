@@ -10,13 +10,16 @@
 // which costs nothing that bounds the kernel (legacy mma.sync: 64 of them per 16 slots and SM are far below its rate).
 //   logits: A = q as bfloat16 terms (one if T is bfloat16, exact; three if float, 24 bits), scaled by a power of two per head.
 //           B = the code's 4 bits as the lowest bits of a bfloat16, a subnormal number code 2^-133: one AND per two codes.
+//           (Four bits further up they are 16 times that, exactly, so only every second nibble needs a shift; the elements of
+//           q that meet those are 16 times smaller.)
 //   values: A = weight x step of the slot as bfloat16 (T bfloat16: rounded, half a step 2^-8, as the output is; float: three
-//           terms), B = the codes as bfloat16 numbers (128 + code by an OR, minus 128).
-// A CTA is 8 warps, each with its own chunks of 16 slots, its own ring of shared-memory stages (cp.async, no barrier between
+//           terms), B = 128 + code as bfloat16 numbers (one AND-OR), the excess 128 sum A taken from one more product with
+//           ones; float subtracts the 128 first, because the difference of the two sums would cost it 4 bits.
+// A CTA is 4 warps, each with its own chunks of 16 slots, its own ring of shared-memory stages (cp.async, no barrier between
 // warps), running maximum, sum and accumulators. Warps are joined through shared memory, the CTAs that share a (sequence,
 // key/value head, block of 16 query heads) through a cluster's distributed shared memory: one launch, no workspace. The
 // maximum that the weights refer to is only raised when it grew by more than 2^8, so the accumulators are hardly ever rescaled.
-// Per-slot weights: the logits go to the weights' own places first and are turned into weights by the lanes that wrote them.
+// Per-slot weights: the logits go to the weights' own places first and are turned into weights by the CTA that wrote them.
 #pragma once
 
 #include <cooperative_groups.h>
@@ -25,7 +28,7 @@
 
 namespace adore {
 
-constexpr int kQ4Warps = 8;
+constexpr int kQ4Warps = 4;
 constexpr int kQ4Threads = 32 * kQ4Warps;
 constexpr int kQ4Chunk = 16;                // slots a warp takes at a time
 constexpr int kQ4Stages = 4;
@@ -74,13 +77,14 @@ __device__ __forceinline__ float q4_exp2(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-// Codes of four pairs of elements as bfloat16 pairs: subnormal (code 2^-133), or the numbers themselves.
-__device__ __forceinline__ uint32_t q4_tiny(uint32_t w, int n) { return (w >> (4 * n)) & 0x000f000fu; }
+// Codes n (0..3) of a word's two halves as bfloat16 pairs: code 2^-133 (n even) or code 2^-129 (n odd).
+__device__ __forceinline__ uint32_t q4_tiny(uint32_t w, int n) { return (n & 2 ? w >> 8 : w) & (n & 1 ? 0x00f000f0u : 0x000f000fu); }
+// 128 + code, or with EXACT the code itself.
+template <bool EXACT>
 __device__ __forceinline__ uint32_t q4_number(uint32_t w, int n) {
-  uint32_t r;
-  const uint32_t x = ((w >> (4 * n)) & 0x000f000fu) | 0x43004300u;      // 128 + code
-  asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(x), "r"(0x43004300u));
-  return r;
+  uint32_t x = ((w >> (4 * n)) & 0x000f000fu) | 0x43004300u;
+  if (EXACT) asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(x) : "r"(x), "r"(0x43004300u));
+  return x;
 }
 
 // Words of one lane's piece.
@@ -97,7 +101,7 @@ __device__ __forceinline__ void q4_lds(const void* p, uint32_t (&w)[N]) {
 
 // HB: query heads of a block, 8 or 16 (8: rows 8..15 of the matrix instructions are empty).
 template <typename T, int DH, int HB>
-__global__ void __launch_bounds__(kQ4Threads, 2)
+__global__ void __launch_bounds__(kQ4Threads, 4)
 q4_attention_kernel(const Q4Rows c, int H, int Hk, int C, int P, int blocks, int ctas, float scale, const T* q, const T* k_new, const T* v_new,
                     const int* slot_pos, T* out, float* weights) {
   using S = Q4Smem<DH>;
@@ -122,31 +126,33 @@ q4_attention_kernel(const Q4Rows c, int H, int Hk, int C, int P, int blocks, int
   const float to_log2 = scale * 1.4426950408889634f;
 
   // ---- loads of a chunk into a stage of this warp's ring
-  const int chunks = P / kQ4Chunk, step = ctas * kQ4Warps;
+  const int chunks = P / kQ4Chunk, step = ctas * kQ4Warps, first = rank * kQ4Warps + warp;
   unsigned char* ring = q4_smem + warp * (kQ4Stages * S::kStageBytes);
-  auto load = [&](int chunk, int stage) {
-    if (chunk < chunks) {
-      unsigned char* d = ring + stage * S::kStageBytes;
-      const size_t at = r * P + size_t(chunk) * kQ4Chunk;
-      const unsigned char* ks = reinterpret_cast<const unsigned char*>(c.k) + at * (DH / 2);
-      const unsigned char* vs = reinterpret_cast<const unsigned char*>(c.v) + at * (DH / 2);
+  constexpr int kPieces = S::kPairBytes / 16;
+  const size_t at = r * P + size_t(first) * kQ4Chunk;
+  const unsigned char* k_src = reinterpret_cast<const unsigned char*>(c.k) + at * (DH / 2) + 16 * lane;
+  const unsigned char* v_src = reinterpret_cast<const unsigned char*>(c.v) + at * (DH / 2) + 16 * lane;
+  const unsigned char* p_src = reinterpret_cast<const unsigned char*>(lane < kPieces ? c.kp : c.vp) + at * (NG * 4) + 16 * (lane % kPieces);
+  const size_t code_step = size_t(step) * S::kCodeBytes, pair_step = size_t(step) * S::kPairBytes;
+  int loading = first;                        // chunk that is loaded next
+  auto load = [&](int stage) {
+    if (loading < chunks) {
+      unsigned char* d = ring + stage * S::kStageBytes + 16 * lane;
 #pragma unroll
       for (int i = 0; i < S::kCodeBytes / 512; ++i) {
-        q4_copy16(d + 512 * i + 16 * lane, ks + 512 * i + 16 * lane);
-        q4_copy16(d + S::kCodeBytes + 512 * i + 16 * lane, vs + 512 * i + 16 * lane);
+        q4_copy16(d + 512 * i, k_src + 512 * i);
+        q4_copy16(d + S::kCodeBytes + 512 * i, v_src + 512 * i);
       }
-      constexpr int kPieces = S::kPairBytes / 16;
-      if (lane < 2 * kPieces) {
-        const int i = lane % kPieces;
-        const unsigned char* src = reinterpret_cast<const unsigned char*>(lane < kPieces ? c.kp : c.vp) + at * (NG * 4) + 16 * i;
-        q4_copy16(d + 2 * S::kCodeBytes + 16 * lane, src);
-      }
+      if (lane < 2 * kPieces) q4_copy16(d + 2 * S::kCodeBytes, p_src);
+      k_src += code_step;
+      v_src += code_step;
+      p_src += pair_step;
+      loading += step;
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
-  const int first = rank * kQ4Warps + warp;
 #pragma unroll
-  for (int i = 0; i < kQ4Stages - 1; ++i) load(first + i * step, i);
+  for (int i = 0; i < kQ4Stages - 1; ++i) load(i);
 
   // ---- queries: bfloat16 fragments, the sums that the low values meet
   uint32_t qa[TERMS == 1 ? DH / 16 : 1][4];
@@ -191,11 +197,12 @@ q4_attention_kernel(const Q4Rows c, int H, int Hk, int C, int P, int blocks, int
     for (int m = 0; m < 2; ++m) {
       // step 2 i + m: k = 2 tig, 2 tig + 1 are elements 2 m, 2 m + 4 of the lane's 8; k + 8 the ones behind them
       uint32_t t0[TERMS], t1[TERMS] = {}, t2[TERMS], t3[TERMS] = {};
+      // (the latter meet codes 2^-129 instead of 2^-133)
       q4_terms<TERMS>(qx[0][i][2 * m], qx[0][i][2 * m + 4], t0);
-      q4_terms<TERMS>(qx[0][i][2 * m + 1], qx[0][i][2 * m + 5], t2);
+      q4_terms<TERMS>(qx[0][i][2 * m + 1] * 0.0625f, qx[0][i][2 * m + 5] * 0.0625f, t2);
       if (NR == 2) {
         q4_terms<TERMS>(qx[NR - 1][i][2 * m], qx[NR - 1][i][2 * m + 4], t1);
-        q4_terms<TERMS>(qx[NR - 1][i][2 * m + 1], qx[NR - 1][i][2 * m + 5], t3);
+        q4_terms<TERMS>(qx[NR - 1][i][2 * m + 1] * 0.0625f, qx[NR - 1][i][2 * m + 5] * 0.0625f, t3);
       }
       if constexpr (TERMS == 1) {
         qa[2 * i + m][0] = t0[0]; qa[2 * i + m][1] = t1[0]; qa[2 * i + m][2] = t2[0]; qa[2 * i + m][3] = t3[0];
@@ -218,7 +225,9 @@ q4_attention_kernel(const Q4Rows c, int H, int Hk, int C, int P, int blocks, int
 
   // ---- this warp's chunks
   float o[DH / 8][4];
-  float m[NR], l[NR], low_acc[NR][NG];
+  float m[NR], l[NR], low_acc[NR][NG], excess[NG][4];
+#pragma unroll
+  for (int n = 0; n < NG; ++n) excess[n][0] = excess[n][1] = excess[n][2] = excess[n][3] = 0.f;
 #pragma unroll
   for (int i = 0; i < DH / 8; ++i)
 #pragma unroll
@@ -231,21 +240,18 @@ q4_attention_kernel(const Q4Rows c, int H, int Hk, int C, int P, int blocks, int
     for (int n = 0; n < NG; ++n) low_acc[y][n] = 0.f;
   }
   const int* pos = slot_pos + r * C;
-  auto occupied = [&](int chunk, bool (&have)[2][2]) {
-#pragma unroll
-    for (int nt = 0; nt < 2; ++nt)
-#pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        const int s = chunk * kQ4Chunk + 8 * nt + 2 * tig + x;
-        have[nt][x] = chunk < chunks && s < C && __ldg(pos + s) >= 0;
-      }
+  // bit j: slot j of the chunk is occupied
+  auto occupied = [&](int chunk) {
+    const int s = chunk * kQ4Chunk + (lane & 15);
+    return chunk < chunks && s < C ? __ldg(pos + s) : -1;
   };
-  bool have[2][2], have_next[2][2];
-  occupied(first, have);
+  int pos_next = occupied(first);
   int stage = 0;
   for (int chunk = first; chunk < chunks; chunk += step) {
-    load(chunk + (kQ4Stages - 1) * step, (stage + kQ4Stages - 1) % kQ4Stages);
-    occupied(chunk + step, have_next);
+    load((stage + kQ4Stages - 1) % kQ4Stages);
+    const unsigned taken = __ballot_sync(0xffffffffu, pos_next >= 0) & 0xffffu;
+    const unsigned mine = taken >> (2 * tig);                // bits 0, 1, 8, 9: this lane's slots
+    pos_next = occupied(chunk + step);
     asm volatile("cp.async.wait_group %0;" ::"n"(kQ4Stages - 1) : "memory");
     __syncwarp();
     const unsigned char* d = ring + stage * S::kStageBytes;
@@ -256,44 +262,53 @@ q4_attention_kernel(const Q4Rows c, int H, int Hk, int C, int P, int blocks, int
       uint32_t w[NW], pair[2 * NG];
       q4_lds<NW>(d + (8 * nt + gid) * (DH / 2) + tig * (4 * NW), w);
       q4_lds<2 * NG>(d + 2 * S::kCodeBytes + (8 * nt + 2 * tig) * (NG * 4), pair);
-#pragma unroll
-      for (int y = 0; y < NR; ++y) x[nt][y][0] = x[nt][y][1] = 0.f;
+      float acc[NG][4];
 #pragma unroll
       for (int n = 0; n < NG; ++n) {
-        float acc[4] = {0.f, 0.f, 0.f, 0.f};
+        acc[n][0] = acc[n][1] = acc[n][2] = acc[n][3] = 0.f;
 #pragma unroll
         for (int i = 2 * n; i < 2 * n + 2; ++i)
 #pragma unroll
           for (int mm = 0; mm < 2; ++mm) {
             const uint32_t b0 = q4_tiny(w[i], 2 * mm), b1 = q4_tiny(w[i], 2 * mm + 1);
             if constexpr (TERMS == 1) {
-              q4_mma(acc, qa[2 * i + mm], b0, b1);
+              q4_mma(acc[n], qa[2 * i + mm], b0, b1);
             } else {
 #pragma unroll
               for (int t = TERMS - 1; t >= 0; --t) {
                 const uint4 f = q_frag[((2 * i + mm) * TERMS + t) * 32 + lane];
                 const uint32_t a[4] = {f.x, f.y, f.z, f.w};
-                q4_mma(acc, a, b0, b1);
+                q4_mma(acc[n], a, b0, b1);
               }
             }
           }
+      }
+#pragma unroll
+      for (int y = 0; y < NR; ++y)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          const float st = q4_low_half(pair[e * NG + n]), lo = q4_high_half(pair[e * NG + n]);
-#pragma unroll
-          for (int y = 0; y < NR; ++y) x[nt][y][e] = fmaf(acc[2 * y + e] * unit_x[y], st, fmaf(lo, qsum[y][n], x[nt][y][e]));
+          float code = acc[0][2 * y + e] * q4_low_half(pair[e * NG]), low = qsum[y][0] * q4_high_half(pair[e * NG]);
+          if (NG == 2) {
+            code = fmaf(acc[NG - 1][2 * y + e], q4_low_half(pair[e * NG + NG - 1]), code);
+            low = fmaf(qsum[y][NG - 1], q4_high_half(pair[e * NG + NG - 1]), low);
+          }
+          x[nt][y][e] = fmaf(code, unit_x[y], low);
         }
-      }
+    }
+    if (taken != 0xffffu) {
+#pragma unroll
+      for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+          if (!(mine >> (8 * nt + e) & 1u)) {
+#pragma unroll
+            for (int y = 0; y < NR; ++y) x[nt][y][e] = -INFINITY;
+          }
     }
     float top[NR];
     bool raise = false;
 #pragma unroll
     for (int y = 0; y < NR; ++y) {
-#pragma unroll
-      for (int nt = 0; nt < 2; ++nt)
-#pragma unroll
-        for (int e = 0; e < 2; ++e)
-          if (!have[nt][e]) x[nt][y][e] = -INFINITY;
       top[y] = fmaxf(fmaxf(x[0][y][0], x[0][y][1]), fmaxf(x[1][y][0], x[1][y][1]));
       raise |= top[y] - m[y] > 8.f;
     }
@@ -306,7 +321,7 @@ q4_attention_kernel(const Q4Rows c, int H, int Hk, int C, int P, int blocks, int
         m[y] = now;
         l[y] *= f;
 #pragma unroll
-        for (int n = 0; n < NG; ++n) low_acc[y][n] *= f;
+        for (int n = 0; n < NG; ++n) { low_acc[y][n] *= f; excess[n][2 * y] *= f; }
 #pragma unroll
         for (int i = 0; i < DH / 8; ++i) { o[i][2 * y] *= f; o[i][2 * y + 1] *= f; }
       }
@@ -338,11 +353,16 @@ q4_attention_kernel(const Q4Rows c, int H, int Hk, int C, int P, int blocks, int
     for (int nt = 0; nt < 2; ++nt) {
       q4_lds<NW>(d + S::kCodeBytes + (4 * nt + tig) * DH + gid * (4 * NW), vw[nt]);
       q4_lds<2 * NG>(d + 2 * S::kCodeBytes + S::kPairBytes + (8 * nt + 2 * tig) * (NG * 4), pair[nt]);
+    }
+    if (taken != 0xffffu) {                   // an empty slot may hold anything
 #pragma unroll
-      for (int e = 0; e < 2; ++e)
+      for (int nt = 0; nt < 2; ++nt)
 #pragma unroll
-        for (int n = 0; n < NG; ++n)
-          if (!have[nt][e]) pair[nt][e * NG + n] = 0u;             // an empty slot may hold anything
+        for (int e = 0; e < 2; ++e)
+          if (!(mine >> (8 * nt + e) & 1u)) {
+#pragma unroll
+            for (int n = 0; n < NG; ++n) pair[nt][e * NG + n] = 0u;
+          }
     }
 #pragma unroll
     for (int n = 0; n < NG; ++n) {
@@ -366,15 +386,12 @@ q4_attention_kernel(const Q4Rows c, int H, int Hk, int C, int P, int blocks, int
       for (int i = 2 * n; i < 2 * n + 2; ++i)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const uint32_t b0 = q4_number(vw[0][i], e), b1 = q4_number(vw[1][i], e);
+          const uint32_t b0 = q4_number<TERMS == 3>(vw[0][i], e), b1 = q4_number<TERMS == 3>(vw[1][i], e);
 #pragma unroll
           for (int z = TERMS - 1; z >= 0; --z) q4_mma(o[4 * i + e], a[z], b0, b1);
         }
+      if constexpr (TERMS == 1) q4_mma(excess[n], a[0], 0x3f803f80u, 0x3f803f80u);      // sums of A
     }
-#pragma unroll
-    for (int nt = 0; nt < 2; ++nt)
-#pragma unroll
-      for (int e = 0; e < 2; ++e) have[nt][e] = have_next[nt][e];
     stage = stage + 1 == kQ4Stages ? 0 : stage + 1;
     __syncwarp();                             // the stage has been read before it is filled again
   }
@@ -393,18 +410,21 @@ q4_attention_kernel(const Q4Rows c, int H, int Hk, int C, int P, int blocks, int
       s_m[warp][gid + 8 * y] = m[y];
       s_l[warp][gid + 8 * y] = l[y];
 #pragma unroll
-      for (int n = 0; n < NG; ++n) s_low[warp][gid + 8 * y][n] = low_acc[y][n];
+      for (int n = 0; n < NG; ++n) s_low[warp][gid + 8 * y][n] = low_acc[y][n] - 128.f * excess[n][2 * y];
     }
   }
   __syncthreads();                            // every warp is done with its ring
   float* part = reinterpret_cast<float*>(q4_smem);                 // [warp][HB][DH]
 #pragma unroll
-  for (int i = 0; i < DH / 8; ++i)
+  for (int y = 0; y < NR; ++y)
+    if (gid + 8 * y < nh) {
 #pragma unroll
-    for (int y = 0; y < NR; ++y)
+      for (int i = 0; i < NW; ++i)
 #pragma unroll
-      for (int e = 0; e < 2; ++e)             // n-tile 4 w + n, column j: element 32 w + 4 j + n
-        part[(warp * HB + gid + 8 * y) * DH + 32 * (i / 4) + 4 * (2 * tig + e) + i % 4] = o[i][2 * y + e];
+        for (int e = 0; e < 2; ++e)           // n-tile 4 i + n, column j: element 32 i + 4 j + n
+          *reinterpret_cast<float4*>(&part[(warp * HB + gid + 8 * y) * DH + 32 * i + 4 * (2 * tig + e)]) =
+              make_float4(o[4 * i][2 * y + e], o[4 * i + 1][2 * y + e], o[4 * i + 2][2 * y + e], o[4 * i + 3][2 * y + e]);
+    }
   __syncthreads();
   if (threadIdx.x < HB) {
     float top = kQ4Nothing, sum = 0.f;
@@ -414,7 +434,7 @@ q4_attention_kernel(const Q4Rows c, int H, int Hk, int C, int P, int blocks, int
     s_cta_l[threadIdx.x] = sum;
   }
   __syncthreads();
-  for (int i = threadIdx.x; i < HB * DH; i += kQ4Threads) {
+  for (int i = threadIdx.x; i < nh * DH; i += kQ4Threads) {
     const int h = i / DH, e = i % DH;
     float sum = 0.f;
 #pragma unroll
@@ -453,21 +473,15 @@ q4_attention_kernel(const Q4Rows c, int H, int Hk, int C, int P, int blocks, int
     out[(h0 + h) * DH + e] = Elem<T>::from_float(sum * s_inv[h]);
   }
   if (weights != nullptr) {
-#pragma unroll
-    for (int y = 0; y < NR; ++y) {
-      const int h = gid + 8 * y;
-      if (h >= nh) continue;
+    // this CTA's slots, 16 per warp side by side, logits to weights (written by this CTA before its barriers above)
+    for (int h = 0; h < nh; ++h) {
       float* row = weights + (h0 + h) * (size_t(C) + 1);
       const float top = s_top[h], inv = s_inv[h];
-      for (int chunk = first; chunk < chunks; chunk += step)
-#pragma unroll
-        for (int nt = 0; nt < 2; ++nt)
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const int s = chunk * kQ4Chunk + 8 * nt + 2 * tig + e;
-            if (s < C) row[s] = q4_exp2(row[s] - top) * inv;
-          }
-      if (rank == 0 && warp == 0 && tig == 0) row[C] = s_l[0][h] * inv;
+      for (int chunk = rank * kQ4Warps; chunk < chunks; chunk += step) {
+        const int s = chunk * kQ4Chunk + threadIdx.x;
+        if (threadIdx.x < kQ4Warps * kQ4Chunk && s < C) row[s] = q4_exp2(row[s] - top) * inv;
+      }
+      if (rank == 0 && threadIdx.x == 0) row[C] = s_l[0][h] * inv;
     }
   }
   if (ctas > 1) cluster.sync();               // nobody leaves while its shared memory is read

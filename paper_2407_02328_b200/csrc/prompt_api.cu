@@ -222,12 +222,12 @@ int q4_split(int64_t units, int chunks, int sms) {
   return best;
 }
 
-template <typename T, int DH, int HB>
+template <typename T, int DH, int NB>
 adore_status_t attend_q4_as(const adore_q4_t* c, const void* q, const void* k, const void* v, const Q4Rows& rows, const int* slot_pos, void* out,
                             float* weights, cudaStream_t st) {
-  auto kernel = q4_attention_kernel<T, DH, HB>;
-  constexpr size_t smem = q4_attention_smem<T, DH, HB>();
-  const int P = q4_padded(c->capacity), blocks = (c->n_heads / c->n_kv_heads + HB - 1) / HB;
+  auto kernel = q4_attention_kernel<T, DH, NB>;
+  constexpr size_t smem = q4_attention_smem<T, DH, NB>();
+  const int P = q4_padded(c->capacity), blocks = (c->n_heads / c->n_kv_heads + 8 * NB - 1) / (8 * NB);
   const int64_t units = int64_t(c->batch) * c->n_kv_heads * blocks;
   const int ctas = q4_split(units, P / kQ4Chunk, sm_count());
   if (units * ctas > kMaxGrid) return ADORE_ERR_UNSUPPORTED;
@@ -248,8 +248,8 @@ adore_status_t attend_q4_as(const adore_q4_t* c, const void* q, const void* k, c
 template <typename T, int DH>
 adore_status_t attend_q4(const adore_q4_t* c, const void* q, const void* k, const void* v, const Q4Rows& rows, const int* slot_pos, void* out,
                          float* weights, cudaStream_t st) {
-  return c->n_heads / c->n_kv_heads <= 8 ? attend_q4_as<T, DH, 8>(c, q, k, v, rows, slot_pos, out, weights, st)
-                                         : attend_q4_as<T, DH, 16>(c, q, k, v, rows, slot_pos, out, weights, st);
+  return c->n_heads / c->n_kv_heads <= 8 ? attend_q4_as<T, DH, 1>(c, q, k, v, rows, slot_pos, out, weights, st)
+                                         : attend_q4_as<T, DH, 2>(c, q, k, v, rows, slot_pos, out, weights, st);
 }
 
 template <typename T, int DH>

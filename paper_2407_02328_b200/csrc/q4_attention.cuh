@@ -4,17 +4,17 @@
 //   out = sum_s softmax(x)_s (code_s step_s + low_s)
 //
 // Bound by reading the rows: 144 bytes per slot and key/value head at dh = 128 (72 at 64). The codes go into the matrix
-// instructions as they are, so that no element is ever expanded to a full value: with B = codes of 8 slots x 16 elements
-// and A = up to 16 query heads, one mma.m16n8k16 gives 128 partial logits; step and low are applied per slot and group to its
-// result. Query heads of a key/value head share the rows; with 8 or fewer heads half of the instruction's rows stay empty,
-// which costs nothing that bounds the kernel (legacy mma.sync: 64 of them per 16 slots and SM are far below its rate).
-//   logits: A = q as bfloat16 terms (one if T is bfloat16, exact; three if float, 24 bits), scaled by a power of two per head.
-//           B = the code's 4 bits as the lowest bits of a bfloat16, a subnormal number code 2^-133: one AND per two codes.
-//           (Four bits further up they are 16 times that, exactly, so only every second nibble needs a shift; the elements of
-//           q that meet those are 16 times smaller.)
-//   values: A = weight x step of the slot as bfloat16 (T bfloat16: rounded, half a step 2^-8, as the output is; float: three
-//           terms), B = 128 + code as bfloat16 numbers (one AND-OR), the excess 128 sum A taken from one more product with
-//           ones; float subtracts the 128 first, because the difference of the two sums would cost it 4 bits.
+// instructions (mma.m16n8k16) as they are, so that no element is ever expanded to a full value; step and low are applied per
+// slot and group to the result. The rows of the cache are the 16 rows of A, up to 8 query heads of the key/value head the
+// columns of B (16 heads: two products with the same A), so that few heads waste no instructions:
+//   logits: A = codes of 16 slots x 16 elements, the 4 bits as the lowest bits of a bfloat16, a subnormal number code 2^-133:
+//           one AND per two codes. (Four bits further up they are 16 times that, exactly, so only every second nibble needs
+//           a shift; the elements of q that meet those are 16 times smaller.) B = q as bfloat16 terms (one if T is bfloat16,
+//           exact; three if float, 24 bits), scaled by a power of two per head.
+//   values: A = codes of 16 elements x 16 slots as 128 + code (one AND-OR), B = weight x step of the slot as bfloat16
+//           (T bfloat16: rounded, half a step 2^-8, as the output is; float: three terms), brought from the logits' layout to
+//           B's by movmatrix. The excess 128 sum B comes from one more product with ones; float subtracts the 128 first,
+//           because the difference of the two sums would cost it 4 bits.
 // A CTA is 4 warps, each with its own chunks of 16 slots, its own ring of shared-memory stages (cp.async, no barrier between
 // warps), running maximum, sum and accumulators. Warps are joined through shared memory, the CTAs that share a (sequence,
 // key/value head, block of 16 query heads) through a cluster's distributed shared memory: one launch, no workspace. The
@@ -41,19 +41,25 @@ struct Q4Smem {
   static constexpr int kStageBytes = 2 * kCodeBytes + 2 * kPairBytes;
   static constexpr int kRing = kQ4Warps * kQ4Stages * kStageBytes;
 };
-template <typename T, int DH, int HB>
+template <typename T, int DH, int NB>
 __host__ __device__ constexpr size_t q4_attention_smem() {
   // the ring, later the warps' accumulators; the query fragments of float heads
-  const size_t ring = Q4Smem<DH>::kRing, acc = size_t(kQ4Warps) * HB * DH * 4;
-  return (ring > acc ? ring : acc) + (sizeof(T) == 4 ? size_t(DH / 16) * 3 * 32 * 16 : 0);
+  const size_t ring = Q4Smem<DH>::kRing, acc = size_t(kQ4Warps) * 8 * NB * DH * 4;
+  return (ring > acc ? ring : acc) + (sizeof(T) == 4 ? size_t(NB) * (DH / 16) * 3 * 32 * 8 : 0);
 }
 
 __device__ __forceinline__ void q4_copy16(void* dst, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(static_cast<uint32_t>(__cvta_generic_to_shared(dst))), "l"(src) : "memory");
 }
-__device__ __forceinline__ void q4_mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+__device__ __forceinline__ void q4_mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// 8 x 8 16-bit matrix, row gid and columns 2 tig, 2 tig + 1 in a lane: transposed.
+__device__ __forceinline__ uint32_t q4_transpose(uint32_t x) {
+  uint32_t y;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
 }
 __device__ __forceinline__ uint32_t q4_bf16x2(float lo, float hi) {
   uint32_t r;
@@ -90,7 +96,9 @@ __device__ __forceinline__ uint32_t q4_number(uint32_t w, int n) {
 // Words of one lane's piece.
 template <int N>
 __device__ __forceinline__ void q4_lds(const void* p, uint32_t (&w)[N]) {
-  if constexpr (N == 4) {
+  if constexpr (N == 1) {
+    w[0] = *static_cast<const uint32_t*>(p);
+  } else if constexpr (N == 4) {
     const uint4 x = *static_cast<const uint4*>(p);
     w[0] = x.x; w[1] = x.y; w[2] = x.z; w[3] = x.w;
   } else {
@@ -99,8 +107,8 @@ __device__ __forceinline__ void q4_lds(const void* p, uint32_t (&w)[N]) {
   }
 }
 
-// HB: query heads of a block, 8 or 16 (8: rows 8..15 of the matrix instructions are empty).
-template <typename T, int DH, int HB>
+// NB: blocks of 8 query heads, 1 or 2.
+template <typename T, int DH, int NB>
 __global__ void __launch_bounds__(kQ4Threads, 4)
 q4_attention_kernel(const Q4Rows c, int H, int Hk, int C, int P, int blocks, int ctas, float scale, const T* q, const T* k_new, const T* v_new,
                     const int* slot_pos, T* out, float* weights) {
@@ -108,9 +116,9 @@ q4_attention_kernel(const Q4Rows c, int H, int Hk, int C, int P, int blocks, int
   constexpr int TERMS = sizeof(T) == 4 ? 3 : 1;
   constexpr int NW = DH / 32;                 // words of a lane's piece of a row
   constexpr int NG = DH / kQ4Group;
-  constexpr int NR = HB / 8;                  // accumulator rows of a lane that hold heads
+  constexpr int HB = 8 * NB;
   extern __shared__ __align__(16) unsigned char q4_smem[];
-  uint4* q_frag = reinterpret_cast<uint4*>(q4_smem + (q4_attention_smem<T, DH, HB>() - (TERMS == 3 ? size_t(DH / 16) * 3 * 32 * 16 : 0)));
+  uint2* q_frag = reinterpret_cast<uint2*>(q4_smem + (q4_attention_smem<T, DH, NB>() - (TERMS == 3 ? size_t(NB) * (DH / 16) * 3 * 32 * 8 : 0)));
   __shared__ float s_m[kQ4Warps][HB], s_l[kQ4Warps][HB], s_low[kQ4Warps][HB][NG];
   __shared__ float s_new[HB];                 // logits of the token's own row (log 2 units)
   __shared__ float s_cta_m[HB], s_cta_l[HB];  // this CTA's, read by the cluster
@@ -154,63 +162,63 @@ q4_attention_kernel(const Q4Rows c, int H, int Hk, int C, int P, int blocks, int
 #pragma unroll
   for (int i = 0; i < kQ4Stages - 1; ++i) load(i);
 
-  // ---- queries: bfloat16 fragments, the sums that the low values meet
-  uint32_t qa[TERMS == 1 ? DH / 16 : 1][4];
-  float qsum[NR][NG], unit_x[NR];
-  float qx[NR][NW][8];
+  // ---- queries: bfloat16 fragments (B: column gid is head 8 y + gid), the sums that the low values meet
+  uint32_t qb[TERMS == 1 ? NB : 1][TERMS == 1 ? DH / 16 : 1][2];
+  float qsum[NB][2][NG], unit_x[NB][2];       // of heads 8 y + 2 tig and the next, this lane's columns of the logits
 #pragma unroll
-  for (int y = 0; y < NR; ++y) {
-    const bool have = gid + 8 * y < nh;
-    float top = 0.f;
+  for (int y = 0; y < NB; ++y) {
+    float x[NW][8], top = 0.f, sum[NG];
+    const bool have = 8 * y + gid < nh;
 #pragma unroll
-    for (int n = 0; n < NG; ++n) qsum[y][n] = 0.f;
+    for (int n = 0; n < NG; ++n) sum[n] = 0.f;
 #pragma unroll
     for (int i = 0; i < NW; ++i) {
-      if (have) load8(q + (h0 + gid + 8 * y) * DH + 32 * i + 8 * tig, qx[y][i]);
+      if (have) load8(q + (h0 + 8 * y + gid) * DH + 32 * i + 8 * tig, x[i]);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        if (!have) qx[y][i][e] = 0.f;
-        top = fmaxf(top, fabsf(qx[y][i][e]));
-        qsum[y][i / 2] += qx[y][i][e];
+        if (!have) x[i][e] = 0.f;
+        top = fmaxf(top, fabsf(x[i][e]));
+        sum[i / 2] += x[i][e];
       }
     }
 #pragma unroll
     for (int o = 1; o < 4; o <<= 1) {
       top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
 #pragma unroll
-      for (int n = 0; n < NG; ++n) qsum[y][n] += __shfl_xor_sync(0xffffffffu, qsum[y][n], o);
+      for (int n = 0; n < NG; ++n) sum[n] += __shfl_xor_sync(0xffffffffu, sum[n], o);
     }
     // largest element to [1, 2) 2^126; a code is 2^-133, so a product is 2^-7 of the plain one
     const int e2 = max(-120, min(120, (int(__float_as_uint(top) >> 23) & 255) - 127));
     const float to_unit = __uint_as_float(uint32_t(127 - e2) << 23);
+    const float from_unit = to_log2 * 128.f * __uint_as_float(uint32_t(127 + e2) << 23);
 #pragma unroll
-    for (int i = 0; i < NW; ++i)
+    for (int e = 0; e < 2; ++e) {
+      const int src = 4 * (2 * tig + e);      // a lane whose gid is this lane's column
+      unit_x[y][e] = __shfl_sync(0xffffffffu, from_unit, src);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) qx[y][i][e] = qx[y][i][e] * to_unit * 8.507059173023462e37f;      // 2^126
-    unit_x[y] = to_log2 * 128.f * __uint_as_float(uint32_t(127 + e2) << 23);
+      for (int n = 0; n < NG; ++n) qsum[y][e][n] = __shfl_sync(0xffffffffu, sum[n], src) * to_log2;
+    }
 #pragma unroll
-    for (int n = 0; n < NG; ++n) qsum[y][n] *= to_log2;
-  }
+    for (int i = 0; i < NW; ++i) {
 #pragma unroll
-  for (int i = 0; i < NW; ++i)
+      for (int e = 0; e < 8; ++e) x[i][e] = x[i][e] * to_unit * 8.507059173023462e37f;      // 2^126
 #pragma unroll
-    for (int m = 0; m < 2; ++m) {
-      // step 2 i + m: k = 2 tig, 2 tig + 1 are elements 2 m, 2 m + 4 of the lane's 8; k + 8 the ones behind them
-      uint32_t t0[TERMS], t1[TERMS] = {}, t2[TERMS], t3[TERMS] = {};
-      // (the latter meet codes 2^-129 instead of 2^-133)
-      q4_terms<TERMS>(qx[0][i][2 * m], qx[0][i][2 * m + 4], t0);
-      q4_terms<TERMS>(qx[0][i][2 * m + 1] * 0.0625f, qx[0][i][2 * m + 5] * 0.0625f, t2);
-      if (NR == 2) {
-        q4_terms<TERMS>(qx[NR - 1][i][2 * m], qx[NR - 1][i][2 * m + 4], t1);
-        q4_terms<TERMS>(qx[NR - 1][i][2 * m + 1] * 0.0625f, qx[NR - 1][i][2 * m + 5] * 0.0625f, t3);
-      }
-      if constexpr (TERMS == 1) {
-        qa[2 * i + m][0] = t0[0]; qa[2 * i + m][1] = t1[0]; qa[2 * i + m][2] = t2[0]; qa[2 * i + m][3] = t3[0];
-      } else if (warp == 0) {
+      for (int m = 0; m < 2; ++m) {
+        // product 2 i + m: k = 2 tig, 2 tig + 1 are elements 2 m, 2 m + 4 of the lane's 8; k + 8 the ones behind them, which
+        // meet codes 2^-129 instead of 2^-133
+        uint32_t t0[TERMS], t1[TERMS];
+        q4_terms<TERMS>(x[i][2 * m], x[i][2 * m + 4], t0);
+        q4_terms<TERMS>(x[i][2 * m + 1] * 0.0625f, x[i][2 * m + 5] * 0.0625f, t1);
+        if constexpr (TERMS == 1) {
+          qb[y][2 * i + m][0] = t0[0];
+          qb[y][2 * i + m][1] = t1[0];
+        } else if (warp == 0) {
 #pragma unroll
-        for (int x = 0; x < TERMS; ++x) q_frag[((2 * i + m) * TERMS + x) * 32 + lane] = make_uint4(t0[x], t1[x], t2[x], t3[x]);
+          for (int z = 0; z < TERMS; ++z) q_frag[((y * (DH / 16) + 2 * i + m) * TERMS + z) * 32 + lane] = make_uint2(t0[z], t1[z]);
+        }
       }
     }
+  }
   if constexpr (TERMS == 3) __syncthreads();
 
   // ---- the token's own row: one warp per head
@@ -224,20 +232,24 @@ q4_attention_kernel(const Q4Rows c, int H, int Hk, int C, int P, int blocks, int
     }
 
   // ---- this warp's chunks
-  float o[DH / 8][4];
-  float m[NR], l[NR], low_acc[NR][NG], excess[NG][4];
+  float o[NB][NW][2][4];                      // elements 32 i + 4 gid + 2 j (and + 1) of heads 2 tig, 2 tig + 1
+  float m[NB][2], l[NB][2], low_acc[NB][2][NG], excess[NB][NG][4];
 #pragma unroll
-  for (int n = 0; n < NG; ++n) excess[n][0] = excess[n][1] = excess[n][2] = excess[n][3] = 0.f;
+  for (int y = 0; y < NB; ++y) {
 #pragma unroll
-  for (int i = 0; i < DH / 8; ++i)
+    for (int x = 0; x < 4; ++x) {
 #pragma unroll
-    for (int x = 0; x < 4; ++x) o[i][x] = 0.f;
+      for (int i = 0; i < NW; ++i) o[y][i][0][x] = o[y][i][1][x] = 0.f;
 #pragma unroll
-  for (int y = 0; y < NR; ++y) {
-    m[y] = kQ4Nothing;
-    l[y] = 0.f;
+      for (int n = 0; n < NG; ++n) excess[y][n][x] = 0.f;
+    }
 #pragma unroll
-    for (int n = 0; n < NG; ++n) low_acc[y][n] = 0.f;
+    for (int e = 0; e < 2; ++e) {
+      m[y][e] = kQ4Nothing;
+      l[y][e] = 0.f;
+#pragma unroll
+      for (int n = 0; n < NG; ++n) low_acc[y][e][n] = 0.f;
+    }
   }
   const int* pos = slot_pos + r * C;
   // bit j: slot j of the chunk is occupied
@@ -246,151 +258,148 @@ q4_attention_kernel(const Q4Rows c, int H, int Hk, int C, int P, int blocks, int
     return chunk < chunks && s < C ? __ldg(pos + s) : -1;
   };
   int pos_next = occupied(first);
+  float* w_row = weights != nullptr ? weights + (h0 + 2 * tig) * (size_t(C) + 1) + size_t(first) * kQ4Chunk + gid : nullptr;
   int stage = 0;
   for (int chunk = first; chunk < chunks; chunk += step) {
     load((stage + kQ4Stages - 1) % kQ4Stages);
     const unsigned taken = __ballot_sync(0xffffffffu, pos_next >= 0) & 0xffffu;
-    const unsigned mine = taken >> (2 * tig);                // bits 0, 1, 8, 9: this lane's slots
     pos_next = occupied(chunk + step);
     asm volatile("cp.async.wait_group %0;" ::"n"(kQ4Stages - 1) : "memory");
     __syncwarp();
     const unsigned char* d = ring + stage * S::kStageBytes;
-    // logits of 2 x 8 slots: this lane's are slots 2 tig, 2 tig + 1 of heads gid (and gid + 8)
-    float x[2][NR][2];
+    const bool have[2] = {(taken >> gid & 1u) != 0u, (taken >> (gid + 8) & 1u) != 0u};
+    // logits: slots gid and gid + 8 of heads 8 y + 2 tig, 8 y + 2 tig + 1
+    float x[NB][2][2];
+    {
+      uint32_t w[2][NW], pair[2][NG];
 #pragma unroll
-    for (int nt = 0; nt < 2; ++nt) {
-      uint32_t w[NW], pair[2 * NG];
-      q4_lds<NW>(d + (8 * nt + gid) * (DH / 2) + tig * (4 * NW), w);
-      q4_lds<2 * NG>(d + 2 * S::kCodeBytes + (8 * nt + 2 * tig) * (NG * 4), pair);
-      float acc[NG][4];
+      for (int u = 0; u < 2; ++u) {
+        q4_lds<NW>(d + (8 * u + gid) * (DH / 2) + tig * (4 * NW), w[u]);
+        q4_lds<NG>(d + 2 * S::kCodeBytes + (8 * u + gid) * (NG * 4), pair[u]);
+      }
+      float acc[NB][NG][4];
 #pragma unroll
-      for (int n = 0; n < NG; ++n) {
-        acc[n][0] = acc[n][1] = acc[n][2] = acc[n][3] = 0.f;
+      for (int y = 0; y < NB; ++y)
 #pragma unroll
-        for (int i = 2 * n; i < 2 * n + 2; ++i)
+        for (int n = 0; n < NG; ++n) acc[y][n][0] = acc[y][n][1] = acc[y][n][2] = acc[y][n][3] = 0.f;
 #pragma unroll
-          for (int mm = 0; mm < 2; ++mm) {
-            const uint32_t b0 = q4_tiny(w[i], 2 * mm), b1 = q4_tiny(w[i], 2 * mm + 1);
+      for (int i = 0; i < NW; ++i)
+#pragma unroll
+        for (int mm = 0; mm < 2; ++mm) {
+          const uint32_t a0 = q4_tiny(w[0][i], 2 * mm), a1 = q4_tiny(w[1][i], 2 * mm);
+          const uint32_t a2 = q4_tiny(w[0][i], 2 * mm + 1), a3 = q4_tiny(w[1][i], 2 * mm + 1);
+#pragma unroll
+          for (int y = 0; y < NB; ++y) {
             if constexpr (TERMS == 1) {
-              q4_mma(acc[n], qa[2 * i + mm], b0, b1);
+              q4_mma(acc[y][i / 2], a0, a1, a2, a3, qb[y][2 * i + mm][0], qb[y][2 * i + mm][1]);
             } else {
 #pragma unroll
-              for (int t = TERMS - 1; t >= 0; --t) {
-                const uint4 f = q_frag[((2 * i + mm) * TERMS + t) * 32 + lane];
-                const uint32_t a[4] = {f.x, f.y, f.z, f.w};
-                q4_mma(acc[n], a, b0, b1);
+              for (int z = TERMS - 1; z >= 0; --z) {
+                const uint2 f = q_frag[((y * (DH / 16) + 2 * i + mm) * TERMS + z) * 32 + lane];
+                q4_mma(acc[y][i / 2], a0, a1, a2, a3, f.x, f.y);
               }
             }
           }
-      }
-#pragma unroll
-      for (int y = 0; y < NR; ++y)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          float code = acc[0][2 * y + e] * q4_low_half(pair[e * NG]), low = qsum[y][0] * q4_high_half(pair[e * NG]);
-          if (NG == 2) {
-            code = fmaf(acc[NG - 1][2 * y + e], q4_low_half(pair[e * NG + NG - 1]), code);
-            low = fmaf(qsum[y][NG - 1], q4_high_half(pair[e * NG + NG - 1]), low);
-          }
-          x[nt][y][e] = fmaf(code, unit_x[y], low);
         }
-    }
-    if (taken != 0xffffu) {
 #pragma unroll
-      for (int nt = 0; nt < 2; ++nt)
+      for (int y = 0; y < NB; ++y)
 #pragma unroll
-        for (int e = 0; e < 2; ++e)
-          if (!(mine >> (8 * nt + e) & 1u)) {
+        for (int u = 0; u < 2; ++u)
 #pragma unroll
-            for (int y = 0; y < NR; ++y) x[nt][y][e] = -INFINITY;
+          for (int e = 0; e < 2; ++e) {
+            float code = acc[y][0][2 * u + e] * q4_low_half(pair[u][0]), low = qsum[y][e][0] * q4_high_half(pair[u][0]);
+            if (NG == 2) {
+              code = fmaf(acc[y][NG - 1][2 * u + e], q4_low_half(pair[u][NG - 1]), code);
+              low = fmaf(qsum[y][e][NG - 1], q4_high_half(pair[u][NG - 1]), low);
+            }
+            x[y][u][e] = have[u] ? fmaf(code, unit_x[y][e], low) : -INFINITY;      // an empty slot may hold anything
           }
     }
-    float top[NR];
     bool raise = false;
 #pragma unroll
-    for (int y = 0; y < NR; ++y) {
-      top[y] = fmaxf(fmaxf(x[0][y][0], x[0][y][1]), fmaxf(x[1][y][0], x[1][y][1]));
-      raise |= top[y] - m[y] > 8.f;
-    }
+    for (int y = 0; y < NB; ++y)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) raise |= fmaxf(x[y][0][e], x[y][1][e]) - m[y][e] > 8.f;
     if (__any_sync(0xffffffffu, raise)) {
 #pragma unroll
-      for (int y = 0; y < NR; ++y) {
+      for (int y = 0; y < NB; ++y)
 #pragma unroll
-        for (int w = 1; w < 4; w <<= 1) top[y] = fmaxf(top[y], __shfl_xor_sync(0xffffffffu, top[y], w));
-        const float now = fmaxf(m[y], top[y]), f = q4_exp2(m[y] - now);
-        m[y] = now;
-        l[y] *= f;
+        for (int e = 0; e < 2; ++e) {
+          float top = fmaxf(x[y][0][e], x[y][1][e]);
 #pragma unroll
-        for (int n = 0; n < NG; ++n) { low_acc[y][n] *= f; excess[n][2 * y] *= f; }
+          for (int w = 4; w < 32; w <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, w));
+          const float now = fmaxf(m[y][e], top), f = q4_exp2(m[y][e] - now);
+          m[y][e] = now;
+          l[y][e] *= f;
 #pragma unroll
-        for (int i = 0; i < DH / 8; ++i) { o[i][2 * y] *= f; o[i][2 * y + 1] *= f; }
-      }
+          for (int n = 0; n < NG; ++n) { low_acc[y][e][n] *= f; excess[y][n][e] *= f; }
+#pragma unroll
+          for (int i = 0; i < NW; ++i) {
+            o[y][i][0][e] *= f; o[y][i][0][2 + e] *= f;
+            o[y][i][1][e] *= f; o[y][i][1][2 + e] *= f;
+          }
+        }
     }
     if (weights != nullptr) {
 #pragma unroll
-      for (int y = 0; y < NR; ++y)
-        if (gid + 8 * y < nh) {
-          float* row = weights + (h0 + gid + 8 * y) * (size_t(C) + 1) + chunk * kQ4Chunk;
-#pragma unroll
-          for (int nt = 0; nt < 2; ++nt)
-#pragma unroll
-            for (int e = 0; e < 2; ++e)
-              if (chunk * kQ4Chunk + 8 * nt + 2 * tig + e < C) row[8 * nt + 2 * tig + e] = x[nt][y][e];
-        }
-    }
-#pragma unroll
-    for (int y = 0; y < NR; ++y)
-#pragma unroll
-      for (int nt = 0; nt < 2; ++nt)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          x[nt][y][e] = q4_exp2(x[nt][y][e] - m[y]);
-          l[y] += x[nt][y][e];
-        }
-    // values: k = slots 2 tig, 2 tig + 1 (nt = 0) and those + 8 (nt = 1)
-    uint32_t vw[2][NW], pair[2][2 * NG];
-#pragma unroll
-    for (int nt = 0; nt < 2; ++nt) {
-      q4_lds<NW>(d + S::kCodeBytes + (4 * nt + tig) * DH + gid * (4 * NW), vw[nt]);
-      q4_lds<2 * NG>(d + 2 * S::kCodeBytes + S::kPairBytes + (8 * nt + 2 * tig) * (NG * 4), pair[nt]);
-    }
-    if (taken != 0xffffu) {                   // an empty slot may hold anything
-#pragma unroll
-      for (int nt = 0; nt < 2; ++nt)
+      for (int y = 0; y < NB; ++y)
 #pragma unroll
         for (int e = 0; e < 2; ++e)
-          if (!(mine >> (8 * nt + e) & 1u)) {
-#pragma unroll
-            for (int n = 0; n < NG; ++n) pair[nt][e * NG + n] = 0u;
+          if (8 * y + 2 * tig + e < nh) {
+            float* row = w_row + (8 * y + e) * (size_t(C) + 1);
+            if (chunk * kQ4Chunk + gid < C) row[0] = x[y][0][e];
+            if (chunk * kQ4Chunk + gid + 8 < C) row[8] = x[y][1][e];
           }
+      w_row += size_t(step) * kQ4Chunk;
+    }
+#pragma unroll
+    for (int y = 0; y < NB; ++y)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        x[y][0][e] = q4_exp2(x[y][0][e] - m[y][e]);
+        x[y][1][e] = q4_exp2(x[y][1][e] - m[y][e]);
+        l[y][e] += x[y][0][e] + x[y][1][e];
+      }
+    // values: k = slots 2 tig, 2 tig + 1 and those + 8
+    uint32_t vw[2][NW], pair[2][NG];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      q4_lds<NW>(d + S::kCodeBytes + (4 * u + tig) * DH + gid * (4 * NW), vw[u]);
+      q4_lds<NG>(d + 2 * S::kCodeBytes + S::kPairBytes + (8 * u + gid) * (NG * 4), pair[u]);
+#pragma unroll
+      for (int n = 0; n < NG; ++n) pair[u][n] = have[u] ? pair[u][n] : 0u;
     }
 #pragma unroll
     for (int n = 0; n < NG; ++n) {
-      uint32_t a[TERMS][4];
+      uint32_t bb[NB][TERMS][2];
 #pragma unroll
-      for (int nt = 0; nt < 2; ++nt) {
-        const float s0 = q4_low_half(pair[nt][n]), s1 = q4_low_half(pair[nt][NG + n]);
-        const float l0 = q4_high_half(pair[nt][n]), l1 = q4_high_half(pair[nt][NG + n]);
+      for (int y = 0; y < NB; ++y)
 #pragma unroll
-        for (int y = 0; y < 2; ++y) {
-          uint32_t t[TERMS] = {};
-          if (y < NR) {
-            q4_terms<TERMS>(x[nt][y < NR ? y : 0][0] * s0, x[nt][y < NR ? y : 0][1] * s1, t);
-            low_acc[y < NR ? y : 0][n] += fmaf(x[nt][y < NR ? y : 0][0], l0, x[nt][y < NR ? y : 0][1] * l1);
-          }
+        for (int u = 0; u < 2; ++u) {
+          const float st = q4_low_half(pair[u][n]), lo = q4_high_half(pair[u][n]);
+          uint32_t t[TERMS];
+          q4_terms<TERMS>(x[y][u][0] * st, x[y][u][1] * st, t);
 #pragma unroll
-          for (int z = 0; z < TERMS; ++z) a[z][2 * nt + y] = t[z];
+          for (int z = 0; z < TERMS; ++z) bb[y][z][u] = q4_transpose(t[z]);
+          low_acc[y][0][n] = fmaf(x[y][u][0], lo, low_acc[y][0][n]);
+          low_acc[y][1][n] = fmaf(x[y][u][1], lo, low_acc[y][1][n]);
         }
-      }
 #pragma unroll
       for (int i = 2 * n; i < 2 * n + 2; ++i)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const uint32_t b0 = q4_number<TERMS == 3>(vw[0][i], e), b1 = q4_number<TERMS == 3>(vw[1][i], e);
+        for (int j = 0; j < 2; ++j) {
+          const uint32_t a0 = q4_number<TERMS == 3>(vw[0][i], 2 * j), a1 = q4_number<TERMS == 3>(vw[0][i], 2 * j + 1);
+          const uint32_t a2 = q4_number<TERMS == 3>(vw[1][i], 2 * j), a3 = q4_number<TERMS == 3>(vw[1][i], 2 * j + 1);
 #pragma unroll
-          for (int z = TERMS - 1; z >= 0; --z) q4_mma(o[4 * i + e], a[z], b0, b1);
+          for (int y = 0; y < NB; ++y)
+#pragma unroll
+            for (int z = TERMS - 1; z >= 0; --z) q4_mma(o[y][i][j], a0, a1, a2, a3, bb[y][z][0], bb[y][z][1]);
         }
-      if constexpr (TERMS == 1) q4_mma(excess[n], a[0], 0x3f803f80u, 0x3f803f80u);      // sums of A
+      if constexpr (TERMS == 1) {
+        constexpr uint32_t one = 0x3f803f80u;
+#pragma unroll
+        for (int y = 0; y < NB; ++y) q4_mma(excess[y][n], one, one, one, one, bb[y][0][0], bb[y][0][1]);      // sums of B
+      }
     }
     stage = stage + 1 == kQ4Stages ? 0 : stage + 1;
     __syncwarp();                             // the stage has been read before it is filled again
@@ -399,32 +408,35 @@ q4_attention_kernel(const Q4Rows c, int H, int Hk, int C, int P, int blocks, int
 
   // ---- join the warps
 #pragma unroll
-  for (int y = 0; y < NR; ++y) {
+  for (int y = 0; y < NB; ++y)
 #pragma unroll
-    for (int w = 1; w < 4; w <<= 1) {
-      l[y] += __shfl_xor_sync(0xffffffffu, l[y], w);
+    for (int e = 0; e < 2; ++e) {
 #pragma unroll
-      for (int n = 0; n < NG; ++n) low_acc[y][n] += __shfl_xor_sync(0xffffffffu, low_acc[y][n], w);
+      for (int w = 4; w < 32; w <<= 1) {
+        l[y][e] += __shfl_xor_sync(0xffffffffu, l[y][e], w);
+#pragma unroll
+        for (int n = 0; n < NG; ++n) low_acc[y][e][n] += __shfl_xor_sync(0xffffffffu, low_acc[y][e][n], w);
+      }
+      if (gid == 0) {
+        const int h = 8 * y + 2 * tig + e;
+        s_m[warp][h] = m[y][e];
+        s_l[warp][h] = l[y][e];
+#pragma unroll
+        for (int n = 0; n < NG; ++n) s_low[warp][h][n] = low_acc[y][e][n] - 128.f * excess[y][n][e];
+      }
     }
-    if (tig == 0) {
-      s_m[warp][gid + 8 * y] = m[y];
-      s_l[warp][gid + 8 * y] = l[y];
-#pragma unroll
-      for (int n = 0; n < NG; ++n) s_low[warp][gid + 8 * y][n] = low_acc[y][n] - 128.f * excess[n][2 * y];
-    }
-  }
   __syncthreads();                            // every warp is done with its ring
   float* part = reinterpret_cast<float*>(q4_smem);                 // [warp][HB][DH]
 #pragma unroll
-  for (int y = 0; y < NR; ++y)
-    if (gid + 8 * y < nh) {
+  for (int y = 0; y < NB; ++y)
 #pragma unroll
-      for (int i = 0; i < NW; ++i)
+    for (int e = 0; e < 2; ++e)
+      if (8 * y + 2 * tig + e < nh) {
 #pragma unroll
-        for (int e = 0; e < 2; ++e)           // n-tile 4 i + n, column j: element 32 i + 4 j + n
-          *reinterpret_cast<float4*>(&part[(warp * HB + gid + 8 * y) * DH + 32 * i + 4 * (2 * tig + e)]) =
-              make_float4(o[4 * i][2 * y + e], o[4 * i + 1][2 * y + e], o[4 * i + 2][2 * y + e], o[4 * i + 3][2 * y + e]);
-    }
+        for (int i = 0; i < NW; ++i)
+          *reinterpret_cast<float4*>(&part[(warp * HB + 8 * y + 2 * tig + e) * DH + 32 * i + 4 * gid]) =
+              make_float4(o[y][i][0][e], o[y][i][0][2 + e], o[y][i][1][e], o[y][i][1][2 + e]);
+      }
   __syncthreads();
   if (threadIdx.x < HB) {
     float top = kQ4Nothing, sum = 0.f;

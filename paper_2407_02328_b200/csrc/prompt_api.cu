@@ -208,48 +208,61 @@ adore_status_t step_rows(const adore_q4_t* c, const float* weights, const void* 
   return launched();
 }
 
-// CTAs that share a (sequence, key/value head, head block): the count n of 1..16 with the least time for the fullest SM. A CTA
-// costs its chunks per warp and about three chunks' time for its start and the joins; an SM's CTAs share the bandwidth, but
-// fewer than three cannot use it up.
-int q4_split(int64_t units, int chunks, int sms) {
-  int best = 1;
+// Warps of a CTA (4 or 8) and CTAs that share a (sequence, key/value head, head block; 1 to 16): the pair with the least time for
+// the fullest SM. A warp costs its chunks and about three chunks' time for its start and the joins; an SM's warps share it, but
+// fewer than twelve cannot use it up. Small CTAs lose less at their joins; with few long rows 8 warps in at most 16 CTAs put
+// more warps to work (3 x 8 rows of 40001 slots: 16 x 4 warps 67 us, 12 x 8 warps 47 us).
+struct Q4Plan { int warps, ctas; };
+Q4Plan q4_plan(int64_t units, int chunks, int sms) {
+  Q4Plan best{4, 1};
   int64_t least = INT64_MAX;
-  for (int n = 1; n <= 16; ++n) {
-    const int64_t on_sm = (units * n + sms - 1) / sms, each = (chunks + kQ4Warps * n - 1) / (kQ4Warps * n) + 3;
-    const int64_t cost = std::max<int64_t>(on_sm, 3) * each;
-    if (cost < least) { least = cost; best = n; }
-  }
+  for (int warps = 4; warps <= 8; warps += 4)
+    for (int n = 1; n <= 16; ++n) {
+      const int64_t on_sm = (units * n + sms - 1) / sms * warps, each = (chunks + warps * n - 1) / (warps * n) + 3;
+      const int64_t cost = std::max<int64_t>(on_sm, 12) * each;
+      if (cost < least) { least = cost; best = Q4Plan{warps, n}; }
+    }
   return best;
 }
 
-template <typename T, int DH, int NB>
-adore_status_t attend_q4_as(const adore_q4_t* c, const void* q, const void* k, const void* v, const Q4Rows& rows, const int* slot_pos, void* out,
-                            float* weights, cudaStream_t st) {
-  auto kernel = q4_attention_kernel<T, DH, NB>;
-  constexpr size_t smem = q4_attention_smem<T, DH, NB>();
-  const int P = q4_padded(c->capacity), blocks = (c->n_heads / c->n_kv_heads + 8 * NB - 1) / (8 * NB);
-  const int64_t units = int64_t(c->batch) * c->n_kv_heads * blocks;
-  const int ctas = q4_split(units, P / kQ4Chunk, sm_count());
-  if (units * ctas > kMaxGrid) return ADORE_ERR_UNSUPPORTED;
+template <typename T, int DH, int NB, int WARPS>
+adore_status_t attend_q4_as(const adore_q4_t* c, int ctas, const void* q, const void* k, const void* v, const Q4Rows& rows,
+                            const int* slot_pos, void* out, float* weights, cudaStream_t st) {
+  auto kernel = q4_attention_kernel<T, DH, NB, WARPS>;
+  constexpr size_t smem = q4_attention_smem<T, DH, NB, WARPS>();
+  const int blocks = (c->n_heads / c->n_kv_heads + 8 * NB - 1) / (8 * NB);
+  const int64_t grid = int64_t(c->batch) * c->n_kv_heads * blocks * ctas;
+  if (grid > kMaxGrid) return ADORE_ERR_UNSUPPORTED;
   if (!allow_smem(kernel, smem)) return ADORE_ERR_CUDA;
-  if (ctas > 8 && cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) { cudaGetLastError(); return ADORE_ERR_CUDA; }
+  if (ctas > 8 && cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) {
+    cudaGetLastError();
+    return ADORE_ERR_CUDA;
+  }
   cudaLaunchConfig_t lc{};
   cudaLaunchAttribute at[1];
   at[0].id = cudaLaunchAttributeClusterDimension;
   at[0].val.clusterDim.x = unsigned(ctas); at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
-  lc.gridDim = dim3(unsigned(units * ctas)); lc.blockDim = dim3(kQ4Threads); lc.dynamicSmemBytes = smem; lc.stream = st;
+  lc.gridDim = dim3(unsigned(grid)); lc.blockDim = dim3(32 * WARPS); lc.dynamicSmemBytes = smem; lc.stream = st;
   lc.attrs = at; lc.numAttrs = ctas > 1 ? 1 : 0;
-  const cudaError_t e = cudaLaunchKernelEx(&lc, kernel, rows, c->n_heads, c->n_kv_heads, c->capacity, P, blocks, ctas, scale_of(c->scale, DH),
-                                           static_cast<const T*>(q), static_cast<const T*>(k), static_cast<const T*>(v), slot_pos,
-                                           static_cast<T*>(out), weights);
+  const cudaError_t e = cudaLaunchKernelEx(&lc, kernel, rows, c->n_heads, c->n_kv_heads, c->capacity, q4_padded(c->capacity), blocks, ctas,
+                                           scale_of(c->scale, DH), static_cast<const T*>(q), static_cast<const T*>(k),
+                                           static_cast<const T*>(v), slot_pos, static_cast<T*>(out), weights);
   if (e != cudaSuccess) { cudaGetLastError(); return ADORE_ERR_CUDA; }
   return launched();
+}
+template <typename T, int DH, int NB>
+adore_status_t attend_q4_by_plan(const adore_q4_t* c, const void* q, const void* k, const void* v, const Q4Rows& rows, const int* slot_pos,
+                                 void* out, float* weights, cudaStream_t st) {
+  const int64_t units = int64_t(c->batch) * c->n_kv_heads * ((c->n_heads / c->n_kv_heads + 8 * NB - 1) / (8 * NB));
+  const Q4Plan plan = q4_plan(units, q4_padded(c->capacity) / kQ4Chunk, sm_count());
+  return plan.warps == 4 ? attend_q4_as<T, DH, NB, 4>(c, plan.ctas, q, k, v, rows, slot_pos, out, weights, st)
+                         : attend_q4_as<T, DH, NB, 8>(c, plan.ctas, q, k, v, rows, slot_pos, out, weights, st);
 }
 template <typename T, int DH>
 adore_status_t attend_q4(const adore_q4_t* c, const void* q, const void* k, const void* v, const Q4Rows& rows, const int* slot_pos, void* out,
                          float* weights, cudaStream_t st) {
-  return c->n_heads / c->n_kv_heads <= 8 ? attend_q4_as<T, DH, 1>(c, q, k, v, rows, slot_pos, out, weights, st)
-                                         : attend_q4_as<T, DH, 2>(c, q, k, v, rows, slot_pos, out, weights, st);
+  return c->n_heads / c->n_kv_heads <= 8 ? attend_q4_by_plan<T, DH, 1>(c, q, k, v, rows, slot_pos, out, weights, st)
+                                         : attend_q4_by_plan<T, DH, 2>(c, q, k, v, rows, slot_pos, out, weights, st);
 }
 
 template <typename T, int DH>

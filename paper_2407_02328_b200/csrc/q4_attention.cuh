@@ -15,7 +15,7 @@
 //           (T bfloat16: rounded, half a step 2^-8, as the output is; float: three terms), brought from the logits' layout to
 //           B's by movmatrix. The excess 128 sum B comes from one more product with ones; float subtracts the 128 first,
 //           because the difference of the two sums would cost it 4 bits.
-// A CTA is 4 warps, each with its own chunks of 16 slots, its own ring of shared-memory stages (cp.async, no barrier between
+// A CTA is 4 or 8 warps, each with its own chunks of 16 slots, its own ring of shared-memory stages (cp.async, no barrier between
 // warps), running maximum, sum and accumulators. Warps are joined through shared memory, the CTAs that share a (sequence,
 // key/value head, block of 16 query heads) through a cluster's distributed shared memory: one launch, no workspace. The
 // maximum that the weights refer to is only raised when it grew by more than 2^8, so the accumulators are hardly ever rescaled.
@@ -28,23 +28,21 @@
 
 namespace adore {
 
-constexpr int kQ4Warps = 4;
-constexpr int kQ4Threads = 32 * kQ4Warps;
 constexpr int kQ4Chunk = 16;                // slots a warp takes at a time
 constexpr int kQ4Stages = 4;
 constexpr float kQ4Nothing = -1e30f;        // running maximum before any slot; finite, so that differences are never NaN
 
-template <int DH>
+template <int DH, int WARPS>
 struct Q4Smem {
   static constexpr int kCodeBytes = kQ4Chunk * DH / 2;
   static constexpr int kPairBytes = kQ4Chunk * (DH / kQ4Group) * 4;
   static constexpr int kStageBytes = 2 * kCodeBytes + 2 * kPairBytes;
-  static constexpr int kRing = kQ4Warps * kQ4Stages * kStageBytes;
+  static constexpr int kRing = WARPS * kQ4Stages * kStageBytes;
 };
-template <typename T, int DH, int NB>
+template <typename T, int DH, int NB, int WARPS>
 __host__ __device__ constexpr size_t q4_attention_smem() {
   // the ring, later the warps' accumulators; the query fragments of float heads
-  const size_t ring = Q4Smem<DH>::kRing, acc = size_t(kQ4Warps) * 8 * NB * DH * 4;
+  const size_t ring = Q4Smem<DH, WARPS>::kRing, acc = size_t(WARPS) * 8 * NB * DH * 4;
   return (ring > acc ? ring : acc) + (sizeof(T) == 4 ? size_t(NB) * (DH / 16) * 3 * 32 * 8 : 0);
 }
 
@@ -107,19 +105,19 @@ __device__ __forceinline__ void q4_lds(const void* p, uint32_t (&w)[N]) {
   }
 }
 
-// NB: blocks of 8 query heads, 1 or 2.
-template <typename T, int DH, int NB>
-__global__ void __launch_bounds__(kQ4Threads, 4)
+// NB: blocks of 8 query heads, 1 or 2. WARPS: 4 or 8; either way 16 warps of 128 registers fill an SM.
+template <typename T, int DH, int NB, int WARPS>
+__global__ void __launch_bounds__(32 * WARPS, 16 / WARPS)
 q4_attention_kernel(const Q4Rows c, int H, int Hk, int C, int P, int blocks, int ctas, float scale, const T* q, const T* k_new, const T* v_new,
                     const int* slot_pos, T* out, float* weights) {
-  using S = Q4Smem<DH>;
+  using S = Q4Smem<DH, WARPS>;
   constexpr int TERMS = sizeof(T) == 4 ? 3 : 1;
   constexpr int NW = DH / 32;                 // words of a lane's piece of a row
   constexpr int NG = DH / kQ4Group;
   constexpr int HB = 8 * NB;
   extern __shared__ __align__(16) unsigned char q4_smem[];
-  uint2* q_frag = reinterpret_cast<uint2*>(q4_smem + (q4_attention_smem<T, DH, NB>() - (TERMS == 3 ? size_t(NB) * (DH / 16) * 3 * 32 * 8 : 0)));
-  __shared__ float s_m[kQ4Warps][HB], s_l[kQ4Warps][HB], s_low[kQ4Warps][HB][NG];
+  uint2* q_frag = reinterpret_cast<uint2*>(q4_smem + (q4_attention_smem<T, DH, NB, WARPS>() - (TERMS == 3 ? size_t(NB) * (DH / 16) * 3 * 32 * 8 : 0)));
+  __shared__ float s_m[WARPS][HB], s_l[WARPS][HB], s_low[WARPS][HB][NG];
   __shared__ float s_new[HB];                 // logits of the token's own row (log 2 units)
   __shared__ float s_cta_m[HB], s_cta_l[HB];  // this CTA's, read by the cluster
   __shared__ float s_scale[16][HB];           // factor of every CTA of the cluster in the result
@@ -134,7 +132,7 @@ q4_attention_kernel(const Q4Rows c, int H, int Hk, int C, int P, int blocks, int
   const float to_log2 = scale * 1.4426950408889634f;
 
   // ---- loads of a chunk into a stage of this warp's ring
-  const int chunks = P / kQ4Chunk, step = ctas * kQ4Warps, first = rank * kQ4Warps + warp;
+  const int chunks = P / kQ4Chunk, step = ctas * WARPS, first = rank * WARPS + warp;
   unsigned char* ring = q4_smem + warp * (kQ4Stages * S::kStageBytes);
   constexpr int kPieces = S::kPairBytes / 16;
   const size_t at = r * P + size_t(first) * kQ4Chunk;
@@ -223,7 +221,7 @@ q4_attention_kernel(const Q4Rows c, int H, int Hk, int C, int P, int blocks, int
 
   // ---- the token's own row: one warp per head
   if (rank == 0)
-    for (int h = warp; h < HB; h += kQ4Warps) {
+    for (int h = warp; h < HB; h += WARPS) {
       float x = 0.f;
       if (k_new != nullptr && h < nh)
         for (int e = lane; e < DH; e += 32) x = fmaf(Elem<T>::to_float(q[(h0 + h) * DH + e]), Elem<T>::to_float(k_new[r * DH + e]), x);
@@ -440,17 +438,17 @@ q4_attention_kernel(const Q4Rows c, int H, int Hk, int C, int P, int blocks, int
   __syncthreads();
   if (threadIdx.x < HB) {
     float top = kQ4Nothing, sum = 0.f;
-    for (int w = 0; w < kQ4Warps; ++w) top = fmaxf(top, s_m[w][threadIdx.x]);
-    for (int w = 0; w < kQ4Warps; ++w) sum += s_l[w][threadIdx.x] * q4_exp2(s_m[w][threadIdx.x] - top);
+    for (int w = 0; w < WARPS; ++w) top = fmaxf(top, s_m[w][threadIdx.x]);
+    for (int w = 0; w < WARPS; ++w) sum += s_l[w][threadIdx.x] * q4_exp2(s_m[w][threadIdx.x] - top);
     s_cta_m[threadIdx.x] = top;
     s_cta_l[threadIdx.x] = sum;
   }
   __syncthreads();
-  for (int i = threadIdx.x; i < nh * DH; i += kQ4Threads) {
+  for (int i = threadIdx.x; i < nh * DH; i += (32 * WARPS)) {
     const int h = i / DH, e = i % DH;
     float sum = 0.f;
 #pragma unroll
-    for (int w = 0; w < kQ4Warps; ++w) sum += (part[(w * HB + h) * DH + e] + s_low[w][h][e / kQ4Group]) * q4_exp2(s_m[w][h] - s_cta_m[h]);
+    for (int w = 0; w < WARPS; ++w) sum += (part[(w * HB + h) * DH + e] + s_low[w][h][e / kQ4Group]) * q4_exp2(s_m[w][h] - s_cta_m[h]);
     part[h * DH + e] = sum;                   // (only this thread reads or writes column e of head h)
   }
 
@@ -477,7 +475,7 @@ q4_attention_kernel(const Q4Rows c, int H, int Hk, int C, int P, int blocks, int
     s_l[0][h] = mine;                         // weight of the token's own row, not yet divided
   }
   __syncthreads();
-  for (int i = rank * kQ4Threads + threadIdx.x; i < nh * DH; i += ctas * kQ4Threads) {
+  for (int i = rank * (32 * WARPS) + threadIdx.x; i < nh * DH; i += ctas * (32 * WARPS)) {
     const int h = i / DH, e = i % DH;
     float sum = 0.f;
     for (int x = 0; x < ctas; ++x) sum += (ctas > 1 ? *cluster.map_shared_rank(&part[i], x) : part[i]) * s_scale[x][h];
@@ -489,9 +487,9 @@ q4_attention_kernel(const Q4Rows c, int H, int Hk, int C, int P, int blocks, int
     for (int h = 0; h < nh; ++h) {
       float* row = weights + (h0 + h) * (size_t(C) + 1);
       const float top = s_top[h], inv = s_inv[h];
-      for (int chunk = rank * kQ4Warps; chunk < chunks; chunk += step) {
+      for (int chunk = rank * WARPS; chunk < chunks; chunk += step) {
         const int s = chunk * kQ4Chunk + threadIdx.x;
-        if (threadIdx.x < kQ4Warps * kQ4Chunk && s < C) row[s] = q4_exp2(row[s] - top) * inv;
+        if (threadIdx.x < WARPS * kQ4Chunk && s < C) row[s] = q4_exp2(row[s] - top) * inv;
       }
       if (rank == 0 && threadIdx.x == 0) row[C] = s_l[0][h] * inv;
     }

@@ -318,109 +318,122 @@ def _refuse(where: str, why: str):
     raise AdoreError(1, f"{where}: {why}")
 
 
-def _tensors(where: str, given) -> None:
-    """given: (name, tensor or None, dtype, shape or None). Contiguous CUDA tensors of the current device, or None."""
+def _torch():
     import torch
-    device = None
+    global _torch, _raw_stream
+    _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    _torch = lambda: torch          # noqa: E731  (an import statement costs a call of a few microseconds a noticeable part)
+    return torch
+
+
+_raw_stream = None
+
+
+def _device(where: str, name: str, t) -> int:
+    """The device of a call: where its first tensor lies, which has to be the current one."""
+    device = t.get_device()
+    if device < 0 or device != _torch().cuda.current_device():
+        _refuse(where, f"{name} is on {t.device}, not on the current device")
+    return device
+
+
+def _stream(cuda_stream, device: int) -> Optional[int]:
+    if cuda_stream is None:
+        cuda_stream = _raw_stream(device) if _raw_stream is not None else _torch().cuda.current_stream().cuda_stream
+    return cuda_stream or None
+
+
+def _tensors(where: str, device: int, given) -> None:
+    """given: (name, tensor or None, dtype, shape): contiguous tensors of the call's device, or None."""
     for name, t, dtype, shape in given:
-        if t is None:
-            continue
-        if t.dtype != dtype:
-            _refuse(where, f"{name} is {t.dtype}, not {dtype}")
-        if t.is_cuda and device is None:
-            device = torch.cuda.current_device()
-        if not t.is_cuda or t.get_device() != device:
-            _refuse(where, f"{name} is on {t.device}, not on the current device")
-        if shape is not None:
+        if t is not None and (t.dtype is not dtype or t.get_device() != device or t.shape != shape or not t.is_contiguous()):
+            if t.dtype is not dtype:
+                _refuse(where, f"{name} is {t.dtype}, not {dtype}")
             if t.shape != shape:
                 _refuse(where, f"{name} has shape {tuple(t.shape)}, not {tuple(shape)}")
-            if not t.is_contiguous():
-                _refuse(where, f"{name} is not contiguous")
+            if t.get_device() != device:
+                _refuse(where, f"{name} is on {t.device}, not on the current device")
+            _refuse(where, f"{name} is not contiguous")
 
 
 def _elem(where: str, t) -> int:
-    import torch
-    if t.dtype == torch.bfloat16:
+    torch = _torch()
+    if t.dtype is torch.bfloat16:
         return ADORE_BF16
-    if t.dtype == torch.float32:
+    if t.dtype is torch.float32:
         return ADORE_F32
     _refuse(where, f"element type {t.dtype}")
-
-
-def _stream(cuda_stream) -> Optional[int]:
-    if cuda_stream is None:
-        import torch
-        cuda_stream = torch.cuda.current_stream().cuda_stream
-    return cuda_stream or None
 
 
 def _at(t) -> Optional[int]:
     return None if t is None else t.data_ptr()
 
 
-def _packed(where: str, seq_start, q, k, v, out, scale: float, n_heads: Optional[int] = None) -> adore_prompt_t:
-    """The shape of packed rows [total, heads, head_dim]; q, v and out may be missing."""
-    import torch
-    if k.dim() != 3 or seq_start.dim() != 1 or seq_start.numel() < 2:
-        _refuse(where, "k is [total, kv_heads, head_dim], seq_start int32 [sequences + 1]")
-    total, hk, dh = k.shape
-    if q is not None:
-        if q.dim() != 3:
-            _refuse(where, "q is [total, heads, head_dim]")
-        n_heads = q.shape[1]
-    p = adore_prompt_t(struct_size=C.sizeof(adore_prompt_t), dtype=_elem(where, k), n_seqs=seq_start.numel() - 1, total=total,
-                       n_heads=n_heads, n_kv_heads=hk, head_dim=dh, scale=scale)
-    for name, t, heads in (("q", q, n_heads), ("k", k, hk), ("v", v, hk), ("out", out, n_heads)):
-        if t is None:
-            continue
-        if t.shape != (total, heads, dh):
-            _refuse(where, f"{name} has shape {tuple(t.shape)}, not {(total, heads, dh)}")
-        if t.stride(2) != 1:
-            _refuse(where, f"the elements of a row of {name} are not consecutive")
-        setattr(p, name + "_row", t.stride(0))
-        setattr(p, name + "_head", t.stride(1))
-    _tensors(where, [("seq_start", seq_start, torch.int32, seq_start.shape)] +
-             [(name, t, k.dtype, None) for name, t in (("q", q), ("k", k), ("v", v), ("out", out))])
-    return p
+def _rows(where: str, name: str, t, dtype, device: int, shape) -> Tuple[int, int]:
+    """Strides of packed rows [total, heads, head_dim]."""
+    if t.shape != shape:
+        _refuse(where, f"{name} has shape {tuple(t.shape)}, not {tuple(shape)}")
+    if t.dtype is not dtype:
+        _refuse(where, f"{name} is {t.dtype}, not {dtype}")
+    if t.get_device() != device:
+        _refuse(where, f"{name} is on {t.device}, not on the current device")
+    row, head, elem = t.stride()
+    if elem != 1:
+        _refuse(where, f"the elements of a row of {name} are not consecutive")
+    return row, head
+
+
+def _packed(where: str, seq_start, q, k, v, out, scale: float):
+    """The shape of packed rows (q, v and out may be missing: as many heads as k then), and their device."""
+    if k.dim() != 3 or seq_start.dim() != 1 or seq_start.numel() < 2 or (q is not None and q.dim() != 3):
+        _refuse(where, "q is [total, heads, head_dim], k [total, kv_heads, head_dim], seq_start int32 [sequences + 1]")
+    total, hk, dh = shape = k.shape
+    h, dtype, device = hk if q is None else q.shape[1], k.dtype, _device(where, "k", k)
+    _tensors(where, device, (("seq_start", seq_start, _torch().int32, seq_start.shape),))
+    k_row, k_head = _rows(where, "k", k, dtype, device, shape)
+    v_row, v_head = (0, 0) if v is None else _rows(where, "v", v, dtype, device, shape)
+    shape = (total, h, dh)
+    q_row, q_head = (0, 0) if q is None else _rows(where, "q", q, dtype, device, shape)
+    out_row, out_head = (0, 0) if out is None else _rows(where, "out", out, dtype, device, shape)
+    return adore_prompt_t(C.sizeof(adore_prompt_t), _elem(where, k), seq_start.shape[0] - 1, total, h, hk, dh, scale, q_row, q_head, k_row,
+                          k_head, v_row, v_head, out_row, out_head), device
 
 
 def adore_prompt_attention(q, k, v, seq_start, out, lse=None, scale: float = 0.0, error_word=None, cuda_stream=None) -> None:
     """Causal attention of packed prompts: q, out [total, heads, dh], k, v [total, kv_heads, dh] (strided rows are fine),
     seq_start int32 [sequences + 1], lse float32 [heads, total] or None, error_word int32 [1] or None."""
-    import torch
-    where = "adore_prompt_attention"
-    p = _packed(where, seq_start, q, k, v, out, scale)
-    _tensors(where, (("lse", lse, torch.float32, (p.n_heads, p.total)), ("error_word", error_word, torch.int32, (1,))))
-    _check(_lib().adore_prompt_attention(C.byref(p), _at(seq_start), _at(q), _at(k), _at(v), _at(out), _at(lse), _at(error_word),
-                                         _stream(cuda_stream)), where)
+    where, torch = "adore_prompt_attention", _torch()
+    p, device = _packed(where, seq_start, q, k, v, out, scale)
+    _tensors(where, device, (("lse", lse, torch.float32, (p.n_heads, p.total)), ("error_word", error_word, torch.int32, (1,))))
+    _check(_lib().adore_prompt_attention(C.byref(p), seq_start.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), _at(lse),
+                                         _at(error_word), _stream(cuda_stream, device)), where)
 
 
 def adore_prompt_weights(q, k, lse, seq_start, acc, window: int = 0, scale: float = 0.0, error_word=None, cuda_stream=None) -> None:
     """Attention weight every prompt token received: acc float32 [kv_heads, total]; window: only the last queries count."""
-    import torch
-    where = "adore_prompt_weights"
-    p = _packed(where, seq_start, q, k, None, None, scale)
-    _tensors(where, (("lse", lse, torch.float32, (p.n_heads, p.total)), ("acc", acc, torch.float32, (p.n_kv_heads, p.total)),
-                     ("error_word", error_word, torch.int32, (1,))))
-    _check(_lib().adore_prompt_weights(C.byref(p), _at(seq_start), _at(q), _at(k), _at(lse), window, _at(acc), _at(error_word),
-                                       _stream(cuda_stream)), where)
+    where, torch = "adore_prompt_weights", _torch()
+    p, device = _packed(where, seq_start, q, k, None, None, scale)
+    _tensors(where, device, (("lse", lse, torch.float32, (p.n_heads, p.total)), ("acc", acc, torch.float32, (p.n_kv_heads, p.total)),
+                             ("error_word", error_word, torch.int32, (1,))))
+    _check(_lib().adore_prompt_weights(C.byref(p), seq_start.data_ptr(), q.data_ptr(), k.data_ptr(), lse.data_ptr(), window, acc.data_ptr(),
+                                       _at(error_word), _stream(cuda_stream, device)), where)
 
 
-def _q4(where: str, like, batch: int, n_heads: int, n_kv_heads: int, head_dim: int, capacity: int, cache, scale: float = 0.0) -> adore_q4_t:
-    import torch
-    c = adore_q4_t(struct_size=C.sizeof(adore_q4_t), dtype=_elem(where, like), batch=batch, n_heads=n_heads, n_kv_heads=n_kv_heads,
-                   head_dim=head_dim, capacity=capacity, scale=scale)
-    _tensors(where, (("cache", cache, torch.uint8, cache.shape),))
+def _q4(where: str, like, batch: int, n_heads: int, n_kv_heads: int, head_dim: int, capacity: int, cache, scale: float = 0.0):
+    """The shape of a cache (heads, dtype as `like`'s), and its device; the buffer has to be large enough."""
+    c = adore_q4_t(C.sizeof(adore_q4_t), _elem(where, like), batch, n_heads, n_kv_heads, head_dim, capacity, scale)
+    device = like.get_device()
+    _tensors(where, device, (("cache", cache, _torch().uint8, cache.shape),))
+    _device(where, "cache", cache)
     need = _lib().adore_q4_bytes(C.byref(c))
-    if need and cache.numel() < need:
+    if cache.numel() < need:
         _refuse(where, f"the cache has {cache.numel()} bytes, {need} are needed")
-    return c
+    return c, device
 
 
 def adore_q4_bytes(batch: int, n_kv_heads: int, head_dim: int, capacity: int) -> int:
     """Bytes of a 4-bit cache buffer (a uint8 tensor)."""
-    c = adore_q4_t(struct_size=C.sizeof(adore_q4_t), dtype=ADORE_BF16, batch=batch, n_heads=n_kv_heads, n_kv_heads=n_kv_heads,
-                   head_dim=head_dim, capacity=capacity, scale=0.0)
+    c = adore_q4_t(C.sizeof(adore_q4_t), ADORE_BF16, batch, n_kv_heads, n_kv_heads, head_dim, capacity, 0.0)
     n = _lib().adore_q4_bytes(C.byref(c))
     if n == 0:
         _refuse("adore_q4_bytes", "shape not supported")
@@ -430,71 +443,67 @@ def adore_q4_bytes(batch: int, n_kv_heads: int, head_dim: int, capacity: int) ->
 def adore_evict_prompt(acc, k, v, seq_start, recent: int, cache, slot_pos, slot_acc, length, error_word=None, cuda_stream=None) -> None:
     """Fills a 4-bit cache from packed prompts: slot_pos int32 and slot_acc float32 [sequences, kv_heads, capacity], length
     int32 [sequences, kv_heads], acc float32 [kv_heads, total] as adore_prompt_weights wrote it."""
-    import torch
-    where = "adore_evict_prompt"
-    p = _packed(where, seq_start, None, k, v, None, 0.0, n_heads=k.shape[1] if k.dim() == 3 else 0)
+    where, torch = "adore_evict_prompt", _torch()
+    p, device = _packed(where, seq_start, None, k, v, None, 0.0)
     if slot_pos.dim() != 3:
         _refuse(where, "slot_pos is int32 [sequences, kv_heads, capacity]")
     shape = (p.n_seqs, p.n_kv_heads, slot_pos.shape[2])
-    c = _q4(where, k, p.n_seqs, p.n_heads, p.n_kv_heads, p.head_dim, shape[2], cache)
-    _tensors(where, (("acc", acc, torch.float32, (p.n_kv_heads, p.total)), ("slot_pos", slot_pos, torch.int32, shape),
-                     ("slot_acc", slot_acc, torch.float32, shape), ("length", length, torch.int32, shape[:2]),
-                     ("error_word", error_word, torch.int32, (1,))))
-    _check(_lib().adore_evict_prompt(C.byref(c), C.byref(p), _at(seq_start), _at(acc), _at(k), _at(v), recent, _at(cache), _at(slot_pos),
-                                     _at(slot_acc), _at(length), _at(error_word), _stream(cuda_stream)), where)
+    c, _ = _q4(where, k, p.n_seqs, p.n_heads, p.n_kv_heads, p.head_dim, shape[2], cache)
+    _tensors(where, device, (("acc", acc, torch.float32, (p.n_kv_heads, p.total)), ("slot_pos", slot_pos, torch.int32, shape),
+                             ("slot_acc", slot_acc, torch.float32, shape), ("length", length, torch.int32, shape[:2]),
+                             ("error_word", error_word, torch.int32, (1,))))
+    _check(_lib().adore_evict_prompt(C.byref(c), C.byref(p), seq_start.data_ptr(), acc.data_ptr(), k.data_ptr(), v.data_ptr(), recent,
+                                     cache.data_ptr(), slot_pos.data_ptr(), slot_acc.data_ptr(), length.data_ptr(), _at(error_word),
+                                     _stream(cuda_stream, device)), where)
 
 
 def adore_evict_step(weights, k_new, v_new, recent: int, cache, slot_pos, slot_acc, length, admit_slot, evicted_pos, error_word=None,
                      cuda_stream=None) -> None:
     """One step's eviction: weights float32 [batch, heads, capacity + 1], k_new, v_new [batch, kv_heads, dh], the state of
     adore_evict_prompt, admit_slot and evicted_pos int32 [batch, kv_heads]."""
-    import torch
-    where = "adore_evict_step"
+    where, torch = "adore_evict_step", _torch()
     if weights.dim() != 3 or k_new.dim() != 3 or slot_pos.dim() != 3:
         _refuse(where, "weights [batch, heads, capacity + 1], k_new [batch, kv_heads, dh], slot_pos [batch, kv_heads, capacity]")
-    b, hk, dh = k_new.shape
-    h, cap = weights.shape[1], slot_pos.shape[2]
-    c = _q4(where, k_new, b, h, hk, dh, cap, cache)
-    _tensors(where, (("weights", weights, torch.float32, (b, h, cap + 1)), ("k_new", k_new, k_new.dtype, (b, hk, dh)),
-                     ("v_new", v_new, k_new.dtype, (b, hk, dh)), ("slot_pos", slot_pos, torch.int32, (b, hk, cap)),
-                     ("slot_acc", slot_acc, torch.float32, (b, hk, cap)), ("length", length, torch.int32, (b, hk)),
-                     ("admit_slot", admit_slot, torch.int32, (b, hk)), ("evicted_pos", evicted_pos, torch.int32, (b, hk)),
-                     ("error_word", error_word, torch.int32, (1,))))
-    _check(_lib().adore_evict_step(C.byref(c), _at(weights), _at(k_new), _at(v_new), recent, _at(cache), _at(slot_pos), _at(slot_acc),
-                                   _at(length), _at(admit_slot), _at(evicted_pos), _at(error_word), _stream(cuda_stream)), where)
+    (b, hk, dh), h, cap, i32, f32, dtype = k_new.shape, weights.shape[1], slot_pos.shape[2], torch.int32, torch.float32, k_new.dtype
+    c, device = _q4(where, k_new, b, h, hk, dh, cap, cache)
+    slots, heads, rows = (b, hk, cap), (b, hk), (b, hk, dh)
+    _tensors(where, device, (("weights", weights, f32, (b, h, cap + 1)), ("k_new", k_new, dtype, rows), ("v_new", v_new, dtype, rows),
+                             ("slot_pos", slot_pos, i32, slots), ("slot_acc", slot_acc, f32, slots), ("length", length, i32, heads),
+                             ("admit_slot", admit_slot, i32, heads), ("evicted_pos", evicted_pos, i32, heads),
+                             ("error_word", error_word, i32, (1,))))
+    _check(_lib().adore_evict_step(C.byref(c), weights.data_ptr(), k_new.data_ptr(), v_new.data_ptr(), recent, cache.data_ptr(),
+                                   slot_pos.data_ptr(), slot_acc.data_ptr(), length.data_ptr(), admit_slot.data_ptr(), evicted_pos.data_ptr(),
+                                   _at(error_word), _stream(cuda_stream, device)), where)
 
 
 def adore_q4_attention(q, k_new, v_new, cache, slot_pos, out, weights=None, scale: float = 0.0, cuda_stream=None) -> None:
     """Decode attention over 4-bit rows: q, out [batch, heads, dh], k_new, v_new [batch, kv_heads, dh] or both None, slot_pos
     int32 [batch, kv_heads, capacity], weights float32 [batch, heads, capacity + 1] or None."""
-    import torch
-    where = "adore_q4_attention"
+    where, torch = "adore_q4_attention", _torch()
     if q.dim() != 3 or slot_pos.dim() != 3:
         _refuse(where, "q [batch, heads, dh], slot_pos [batch, kv_heads, capacity]")
-    b, h, dh = q.shape
-    hk, cap = slot_pos.shape[1:]
-    c = _q4(where, q, b, h, hk, dh, cap, cache, scale)
-    _tensors(where, (("q", q, q.dtype, (b, h, dh)), ("k_new", k_new, q.dtype, (b, hk, dh)), ("v_new", v_new, q.dtype, (b, hk, dh)),
-                     ("slot_pos", slot_pos, torch.int32, (b, hk, cap)), ("out", out, q.dtype, (b, h, dh)),
-                     ("weights", weights, torch.float32, (b, h, cap + 1))))
-    _check(_lib().adore_q4_attention(C.byref(c), _at(q), _at(k_new), _at(v_new), _at(cache), _at(slot_pos), _at(out), _at(weights),
-                                     _stream(cuda_stream)), where)
+    (b, h, dh), (_, hk, cap), dtype = q.shape, slot_pos.shape, q.dtype
+    c, device = _q4(where, q, b, h, hk, dh, cap, cache, scale)
+    _tensors(where, device, (("q", q, dtype, (b, h, dh)), ("k_new", k_new, dtype, (b, hk, dh)), ("v_new", v_new, dtype, (b, hk, dh)),
+                             ("slot_pos", slot_pos, torch.int32, (b, hk, cap)), ("out", out, dtype, (b, h, dh)),
+                             ("weights", weights, torch.float32, (b, h, cap + 1))))
+    _check(_lib().adore_q4_attention(C.byref(c), q.data_ptr(), _at(k_new), _at(v_new), cache.data_ptr(), slot_pos.data_ptr(), out.data_ptr(),
+                                     _at(weights), _stream(cuda_stream, device)), where)
 
 
 def adore_q4_read(cache, capacity: int, slots, k_out, v_out, cuda_stream=None) -> None:
     """The values of cache rows: k_out, v_out [batch, kv_heads, n, dh] of the slots int32 [batch, kv_heads, n] (or, for n = 1,
     [batch, kv_heads]); slots None: all of them in order."""
-    import torch
     where = "adore_q4_read"
     if k_out.dim() != 4:
         _refuse(where, "k_out [batch, kv_heads, n, dh]")
-    b, hk, n, dh = k_out.shape
-    c = _q4(where, k_out, b, hk, hk, dh, capacity, cache)
-    if slots is not None and slots.dim() == 2 and n == 1:
-        slots = slots.unsqueeze(2)
-    _tensors(where, (("slots", slots, torch.int32, (b, hk, n)), ("k_out", k_out, k_out.dtype, k_out.shape),
-                     ("v_out", v_out, k_out.dtype, k_out.shape)))
-    _check(_lib().adore_q4_read(C.byref(c), _at(cache), _at(slots), n, _at(k_out), _at(v_out), _stream(cuda_stream)), where)
+    b, hk, n, dh = shape = k_out.shape
+    c, device = _q4(where, k_out, b, hk, hk, dh, capacity, cache)
+    listed = (b, hk) if slots is not None and n == 1 and slots.dim() == 2 else (b, hk, n)
+    _tensors(where, device, (("slots", slots, _torch().int32, listed), ("k_out", k_out, k_out.dtype, shape),
+                             ("v_out", v_out, k_out.dtype, shape)))
+    _check(_lib().adore_q4_read(C.byref(c), cache.data_ptr(), _at(slots), n, k_out.data_ptr(), v_out.data_ptr(),
+                                _stream(cuda_stream, device)), where)
 
 
 def adore_status_string(status: int) -> str:

@@ -1,5 +1,6 @@
 // Host side of the calls for whole prompts, eviction by attention weight and the 4-bit cache: argument checks and launches.
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 #include <initializer_list>
 
@@ -85,7 +86,7 @@ unsigned tile_grid(const PackedParams& p, int block, int heads) {
 
 // SMs of the current device.
 int sm_count() {
-  static int known[64] = {};
+  static std::atomic<int> known[64] = {};
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) { cudaGetLastError(); return 148; }
   if (known[dev] == 0) {
@@ -98,18 +99,28 @@ int sm_count() {
 
 adore_status_t launched() { return cudaGetLastError() == cudaSuccess ? ADORE_OK : ADORE_ERR_CUDA; }
 
-template <typename K>
-bool allow_smem(K kernel, size_t bytes) {
-  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(bytes)) == cudaSuccess) return true;
-  cudaGetLastError();
-  return false;
+// Allows a kernel its dynamic shared memory (and, with `wide`, clusters of up to 16 CTAs), once per kernel and device.
+template <auto KERNEL>
+bool allow_smem(size_t bytes, bool wide = false) {
+  static std::atomic<uint64_t> done{0};
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) { cudaGetLastError(); return false; }
+  const uint64_t bit = dev >= 0 && dev < 64 ? uint64_t(1) << dev : 0;
+  if (done.load(std::memory_order_relaxed) & bit) return true;
+  if (cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, int(bytes)) != cudaSuccess ||
+      (wide && cudaFuncSetAttribute(KERNEL, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess)) {
+    cudaGetLastError();
+    return false;
+  }
+  done.fetch_or(bit, std::memory_order_relaxed);
+  return true;
 }
 
 template <typename T, int DH>
 adore_status_t attention_simt(const PackedParams& p, const void* q, const void* k, const void* v, void* out, float* lse, cudaStream_t st) {
   const unsigned grid = tile_grid(p, kPsBlock, p.H);
   if (grid == 0) return ADORE_ERR_UNSUPPORTED;
-  if (!allow_smem(prompt_attention_simt_kernel<T, DH>, prompt_simt_smem<DH>())) return ADORE_ERR_CUDA;
+  if (!allow_smem<prompt_attention_simt_kernel<T, DH>>(prompt_simt_smem<DH>())) return ADORE_ERR_CUDA;
   prompt_attention_simt_kernel<T, DH><<<grid, kPsThreads, prompt_simt_smem<DH>(), st>>>(
       p, static_cast<const T*>(q), static_cast<const T*>(k), static_cast<const T*>(v), static_cast<T*>(out), lse);
   return launched();
@@ -119,7 +130,7 @@ template <typename T, int DH>
 adore_status_t weights_simt(const PackedParams& p, const void* q, const void* k, const float* lse, int window, float* acc, cudaStream_t st) {
   const unsigned grid = tile_grid(p, kPsBlock, p.Hk);
   if (grid == 0) return ADORE_ERR_UNSUPPORTED;
-  if (!allow_smem(prompt_weights_simt_kernel<T, DH>, prompt_weights_simt_smem<DH>())) return ADORE_ERR_CUDA;
+  if (!allow_smem<prompt_weights_simt_kernel<T, DH>>(prompt_weights_simt_smem<DH>())) return ADORE_ERR_CUDA;
   prompt_weights_simt_kernel<T, DH><<<grid, kPsThreads, prompt_weights_simt_smem<DH>(), st>>>(
       p, static_cast<const T*>(q), static_cast<const T*>(k), lse, window, acc);
   return launched();
@@ -160,7 +171,7 @@ adore_status_t attention_tc(const PackedParams& p, const void* q, const void* k,
   if (!packed_map(&maps.q, q, p.q_row, p.q_head, p.total, p.H, DH) || !packed_map(&maps.k, k, p.k_row, p.k_head, p.total, p.Hk, DH) ||
       !packed_map(&maps.v, v, p.v_row, p.v_head, p.total, p.Hk, DH))
     return ADORE_ERR_CUDA;
-  if (!allow_smem(prompt_attention_tc_kernel<DH>, PtSmem<DH>::kTotal)) return ADORE_ERR_CUDA;
+  if (!allow_smem<prompt_attention_tc_kernel<DH>>(PtSmem<DH>::kTotal)) return ADORE_ERR_CUDA;
   prompt_attention_tc_kernel<DH><<<grid, kPtThreads, PtSmem<DH>::kTotal, st>>>(maps, p, static_cast<__nv_bfloat16*>(out), lse);
   return launched();
 }
@@ -172,7 +183,7 @@ adore_status_t weights_tc(const PackedParams& p, const void* q, const void* k, c
   PwMaps maps;
   if (!packed_map(&maps.q, q, p.q_row, p.q_head, p.total, p.H, DH) || !packed_map(&maps.k, k, p.k_row, p.k_head, p.total, p.Hk, DH))
     return ADORE_ERR_CUDA;
-  if (!allow_smem(prompt_weights_tc_kernel<DH>, PwSmem<DH>::kTotal)) return ADORE_ERR_CUDA;
+  if (!allow_smem<prompt_weights_tc_kernel<DH>>(PwSmem<DH>::kTotal)) return ADORE_ERR_CUDA;
   prompt_weights_tc_kernel<DH><<<grid, kPwThreads, PwSmem<DH>::kTotal, st>>>(maps, p, lse, window, acc);
   return launched();
 }
@@ -233,11 +244,7 @@ adore_status_t attend_q4_as(const adore_q4_t* c, int ctas, const void* q, const 
   const int blocks = (c->n_heads / c->n_kv_heads + 8 * NB - 1) / (8 * NB);
   const int64_t grid = int64_t(c->batch) * c->n_kv_heads * blocks * ctas;
   if (grid > kMaxGrid) return ADORE_ERR_UNSUPPORTED;
-  if (!allow_smem(kernel, smem)) return ADORE_ERR_CUDA;
-  if (ctas > 8 && cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) {
-    cudaGetLastError();
-    return ADORE_ERR_CUDA;
-  }
+  if (!allow_smem<q4_attention_kernel<T, DH, NB, WARPS>>(smem, true)) return ADORE_ERR_CUDA;
   cudaLaunchConfig_t lc{};
   cudaLaunchAttribute at[1];
   at[0].id = cudaLaunchAttributeClusterDimension;

@@ -7,109 +7,185 @@
 
 namespace adore {
 
-constexpr int kEvictThreads = 512;
-constexpr int kEvictWarps = kEvictThreads / 32;
-
 // Order of values: NaN below every number, both zeros equal.
 __device__ __forceinline__ uint32_t evict_key(float x) {
   if (x != x) return 0u;
   return float_key(x == 0.f ? 0.f : x);
 }
 
-// Exclusive prefix of a flag over the CTA's threads; `total` gets the sum. Two barriers.
-__device__ __forceinline__ int block_rank(bool flag, int* warp_counts, int& total) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const unsigned b = __ballot_sync(0xffffffffu, flag);
-  if (lane == 0) warp_counts[warp] = __popc(b);
+// Sum over the CTA; `slots` has one word per warp and is free again after the next barrier.
+template <int WARPS>
+__device__ __forceinline__ int block_sum(int v, int* slots) {
+  v = __reduce_add_sync(0xffffffffu, v);
+  if ((threadIdx.x & 31) == 0) slots[threadIdx.x >> 5] = v;
   __syncthreads();
-  int mine = lane < kEvictWarps ? warp_counts[lane] : 0;
-  total = warp_sum(mine);
-  const int before = warp_sum(lane < warp ? mine : 0);
-  __syncthreads();
-  return before + __popc(b & ((1u << lane) - 1u));
+  const int lane = threadIdx.x & 31;
+  return __reduce_add_sync(0xffffffffu, lane < WARPS ? slots[lane] : 0);
 }
 
-// Which tokens stay: one CTA per (sequence, key/value head). The threshold is found by a radix select over the older tokens'
-// keys, 8 bits a pass; then one pass in ascending position hands out the slots.
-__global__ void __launch_bounds__(kEvictThreads) evict_select_kernel(const int* seq_start, int total, int Hk, int C, int recent,
-                                                                     const float* acc, int* slot_pos, float* slot_acc, int* length,
-                                                                     unsigned* err) {
-  __shared__ unsigned hist[256];
-  __shared__ unsigned s_prefix, s_need;
-  __shared__ int warp_counts[kEvictWarps];
-  const int s = blockIdx.x / Hk, g = blockIdx.x % Hk;
+// Which tokens stay: one CTA per (sequence, key/value head). The threshold, the need-th largest key of the older tokens, is
+// found bit by bit: a pass counts the keys that are at least the threshold with the next bit set. Each warp owns a
+// contiguous stretch of the row; up to KEYS keys a lane stay in registers for all passes, longer rows are read again. Slots are
+// then handed out in ascending position by ballots, with one sum over the warps before.
+// (Counting needs no atomics: the weights' exponents crowd into few bins of a histogram. 20001 tokens: 57 -> 16 us.)
+template <int THREADS, int KEYS>
+__global__ void __launch_bounds__(THREADS) evict_select_kernel(const int* seq_start, int total, int Hk, int C, int recent, const float* acc,
+                                                               int* slot_pos, float* slot_acc, int* length, unsigned* err) {
+  constexpr int WARPS = THREADS / 32;
+  __shared__ int sums[2][WARPS], before[2][WARPS];
+  const int s = blockIdx.x / Hk, g = blockIdx.x % Hk, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int n = packed_len(seq_start, s, total, err);
   const float* a = acc + size_t(g) * total + (n > 0 ? seq_start[s] : 0);
   int* pos = slot_pos + size_t(blockIdx.x) * C;
   float* val = slot_acc + size_t(blockIdx.x) * C;
   if (threadIdx.x == 0) length[blockIdx.x] = n;
-  const int kept = min(n, C);
-  for (int i = kept + threadIdx.x; i < C; i += kEvictThreads) { pos[i] = -1; val[i] = 0.f; }
+  for (int i = min(n, C) + threadIdx.x; i < C; i += THREADS) { pos[i] = -1; val[i] = 0.f; }
   if (n <= C) {
-    for (int i = threadIdx.x; i < n; i += kEvictThreads) { pos[i] = i; val[i] = a[i]; }
+    for (int i = threadIdx.x; i < n; i += THREADS) { pos[i] = i; val[i] = a[i]; }
     return;
   }
   const int older = n - recent;                 // n > C >= recent
-  unsigned need = unsigned(C - recent), prefix = 0;
-  for (int shift = 24; shift >= 0 && need > 0; shift -= 8) {
-    if (threadIdx.x < 256) hist[threadIdx.x] = 0;
-    __syncthreads();
-    const unsigned mask = shift == 24 ? 0u : ~0u << (shift + 8);
-    for (int i = threadIdx.x; i < older; i += kEvictThreads) {
-      const uint32_t key = evict_key(a[i]);
-      if ((key & mask) == prefix) atomicAdd(&hist[(key >> shift) & 255u], 1u);
-    }
-    __syncthreads();
-    if (threadIdx.x == 0) {
-      unsigned left = need;
-      int d = 255;
-      while (d > 0 && hist[d] < left) left -= hist[d--];
-      s_need = left;
-      s_prefix = prefix | (unsigned(d) << shift);
-    }
-    __syncthreads();
-    need = s_need;
-    prefix = s_prefix;
+  const int need = C - recent;
+  const int per_lane = (n + THREADS - 1) / THREADS, first = warp * per_lane * 32;
+  const bool held = per_lane <= KEYS;
+  // The keys of older tokens; 0 for the others, which is also the key of NaN: thresholds that are counted for are above 0.
+  uint32_t key[KEYS];
+#pragma unroll
+  for (int k = 0; k < KEYS; ++k) {
+    const int i = first + 32 * k + lane;
+    key[k] = held && k < per_lane && i < older ? evict_key(a[i]) : 0u;
   }
-  // keys above `prefix` stay, and of the keys equal to it the first `need`
-  const bool any = C > recent;
-  int ties = 0, out = 0;
-  for (int i0 = 0; i0 < n; i0 += kEvictThreads) {
-    const int i = i0 + threadIdx.x;
-    const float x = i < n ? a[i] : 0.f;
-    const uint32_t key = evict_key(x);
-    const bool old = i < older, tie = old && any && key == prefix;
-    int sum;
-    const int rank = ties + block_rank(tie, warp_counts, sum);
-    ties += sum;
-    const bool keep = i < n && (!old || (any && key > prefix) || (tie && rank < int(need)));
-    const int at = out + block_rank(keep, warp_counts, sum);
-    out += sum;
-    if (keep && at < C) { pos[at] = i; val[at] = x; }
+  auto count_from = [&](uint32_t t) {
+    int c = 0;
+    if (held) {
+#pragma unroll
+      for (int k0 = 0; k0 < KEYS; k0 += 4)
+        if (k0 < per_lane) {
+#pragma unroll
+          for (int k = k0; k < k0 + 4; ++k) c += key[k] >= t;
+        }
+    } else {
+      for (int k = 0; k < per_lane; ++k) {
+        const int i = first + 32 * k + lane;
+        c += i < older && evict_key(a[i]) >= t;
+      }
+    }
+    return c;
+  };
+  uint32_t threshold = 0xffffffffu;             // need == 0: no older token stays
+  int ties = 0;                                 // of the keys equal to the threshold, the first so many stay
+  if (need > 0) {
+    uint32_t t = 0;
+    int at_least = older;                       // keys >= t
+    for (int bit = 31; bit >= 0 && at_least != need; --bit) {
+      const uint32_t next = t | (1u << bit);
+      const int c = block_sum<WARPS>(count_from(next), sums[bit & 1]);
+      if (c >= need) { t = next; at_least = c; }
+    }
+    threshold = t;
+    __syncthreads();
+    int above = 0;
+    if (at_least != need) above = block_sum<WARPS>(t == 0xffffffffu ? 0 : count_from(t + 1), sums[0]);
+    ties = at_least == need ? older : need - above;
+  }
+  __syncthreads();
+  // per warp: keys equal to the threshold, and tokens that stay whatever the ties give
+  int equal = 0, sure = 0;
+  auto look = [&](int k, uint32_t x, bool& eq, bool& in) {
+    const int i = first + 32 * k + lane;
+    eq = i < older && need > 0 && x == threshold;
+    in = i < n && (i >= older || (need > 0 && x > threshold));
+  };
+  auto count_both = [&](int k, uint32_t x) {
+    bool eq, in;
+    look(k, x, eq, in);
+    equal += eq;
+    sure += in;
+  };
+  // (`held` is the same for the whole CTA, and so is the number of stretches: only the first per_lane of the array count)
+  if (held) {
+#pragma unroll
+    for (int k = 0; k < KEYS; ++k)
+      if (k < per_lane) count_both(k, key[k]);
+  } else {
+    for (int k = 0; k < per_lane; ++k) {
+      const int i = first + 32 * k + lane;
+      count_both(k, i < older ? evict_key(a[i]) : 0u);
+    }
+  }
+  equal = __reduce_add_sync(0xffffffffu, equal);
+  sure = __reduce_add_sync(0xffffffffu, sure);
+  if (lane == 0) { sums[0][warp] = equal; sums[1][warp] = sure; }
+  __syncthreads();
+  if (threadIdx.x == 0) {                       // a warp's first tie rank and first slot
+    int e = 0, o = 0;
+    for (int w = 0; w < WARPS; ++w) {
+      before[0][w] = e;
+      before[1][w] = o;
+      o += sums[1][w] + max(0, min(sums[0][w], ties - e));
+      e += sums[0][w];
+    }
+  }
+  __syncthreads();
+  int rank = before[0][warp], out = before[1][warp];
+  const unsigned below = (1u << lane) - 1u;
+  auto place = [&](int k, uint32_t x) {
+    bool eq, in;
+    look(k, x, eq, in);
+    const unsigned eqs = __ballot_sync(0xffffffffu, eq);
+    const bool keep = in || (eq && rank + __popc(eqs & below) < ties);
+    const unsigned keeps = __ballot_sync(0xffffffffu, keep);
+    const int slot = out + __popc(keeps & below), i = first + 32 * k + lane;
+    if (keep && slot < C) { pos[slot] = i; val[slot] = a[i]; }
+    rank += __popc(eqs);
+    out += __popc(keeps);
+  };
+  if (held) {
+#pragma unroll
+    for (int k = 0; k < KEYS; ++k)
+      if (k < per_lane) place(k, key[k]);
+  } else {
+    for (int k = 0; k < per_lane; ++k) {
+      const int i = first + 32 * k + lane;
+      place(k, i < older ? evict_key(a[i]) : 0u);
+    }
   }
 }
 
 // Rows of the kept tokens in 4 bits; empty slots and the padding behind slot C - 1 get zeros. dh / 8 lanes per row.
+// (Bound by the instructions of q4_encode8, so one row per thread and many warps: two or four rows a thread, with their loads in
+// flight together, were slower.)
 template <typename T, int DH>
 __global__ void __launch_bounds__(256) evict_pack_kernel(const PackedParams p, const T* k, const T* v, const int* slot_pos,
                                                          const int* length, int C, int P, const Q4Rows c) {
   constexpr int LPR = DH / 8, ROWS = 256 / LPR;
-  const size_t r = blockIdx.y;
-  const int slot = blockIdx.x * ROWS + threadIdx.x / LPR, j = threadIdx.x % LPR;
+  const int blocks = (P + ROWS - 1) / ROWS;
+  const size_t r = blockIdx.x / blocks;
+  const int slot = int(blockIdx.x % blocks) * ROWS + threadIdx.x / LPR, j = threadIdx.x % LPR;
   const int s = int(r) / p.Hk, g = int(r) % p.Hk;
-  int t = slot < C ? slot_pos[r * C + slot] : -1;
-  if (t >= length[r]) t = -1;
+  const int t = slot < C ? slot_pos[r * C + slot] : -1;
   float kx[8], vx[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) kx[e] = vx[e] = 0.f;
-  if (t >= 0) {
-    const long long row = p.seq_start[s] + t;
+  if (t >= 0 && t < length[r]) {
+    const long long row = (long long)p.seq_start[s] + t;
     load8(k + row * p.k_row + g * p.k_head + 8 * j, kx);
     load8(v + row * p.v_row + g * p.v_head + 8 * j, vx);
   }
   __nv_bfloat162 kpair, vpair;
   const uint32_t kw = q4_encode8(kx, kpair), vw = q4_encode8(vx, vpair);
-  if (slot < P) q4_store_piece<DH>(c, r, P, slot, j, kw, kpair, vw, vpair);
+  // neighbouring slots exchange halves, so that each writes a whole word of the two it shares with the other
+  const uint32_t other = __shfl_xor_sync(0xffffffffu, vw, LPR);
+  if (slot < P) {
+    const bool odd = slot & 1;
+    c.k[(r * P + slot) * (DH / 8) + q4_k_word<DH>(j)] = kw;
+    c.v[(r * (P / 2) + slot / 2) * (DH / 4) + q4_v_word<DH>(j) + (odd ? DH / 32 : 0)] =
+        odd ? (other >> 16) | (vw & 0xffff0000u) : (vw & 0xffffu) | (other << 16);
+    if ((j & 7) == 0) {
+      c.kp[(r * P + slot) * (DH / kQ4Group) + (j >> 3)] = kpair;
+      c.vp[(r * P + slot) * (DH / kQ4Group) + (j >> 3)] = vpair;
+    }
+  }
 }
 
 // One decode step of one (sequence, key/value head): adds the step's weights, picks the slot, writes the new row.
@@ -130,14 +206,35 @@ __global__ void __launch_bounds__(256) evict_step_kernel(const float* weights, c
   const long long newest = (long long)now - recent;
   // (0, slot) of an empty slot < (1, value, slot) of a token that may go < all others
   unsigned long long mine = ~0ull;
-  for (int i = threadIdx.x; i < C; i += 256) {
-    const int at = pos[i];
-    if (at < 0) { mine = min(mine, (unsigned long long)i); continue; }
-    double sum = val[i];
-    for (int h = 0; h < group; ++h) sum += w[h * (size_t(C) + 1) + i];
-    const float x = float(sum);
-    val[i] = x;
-    if (at <= newest) mine = min(mine, (1ull << 63) | ((unsigned long long)evict_key(x) << 31) | unsigned(i));
+  constexpr int U = 4;                          // slots of a thread whose loads are in flight together
+  for (int i0 = threadIdx.x; i0 < C; i0 += 256 * U) {
+    int at[U];
+    float v[U], x[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int i = i0 + 256 * u;
+      at[u] = i < C ? pos[i] : 0;
+      v[u] = i < C ? val[i] : 0.f;
+      x[u] = i < C ? w[i] : 0.f;
+    }
+    double sum[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) sum[u] = double(x[u]);
+    for (int h = 1; h < group; ++h) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) x[u] = i0 + 256 * u < C ? w[h * (size_t(C) + 1) + i0 + 256 * u] : 0.f;
+#pragma unroll
+      for (int u = 0; u < U; ++u) sum[u] += double(x[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int i = i0 + 256 * u;
+      if (i >= C) break;
+      if (at[u] < 0) { mine = min(mine, (unsigned long long)i); continue; }
+      const float now_worth = float(double(v[u]) + sum[u]);
+      val[i] = now_worth;
+      if (at[u] <= newest) mine = min(mine, (1ull << 63) | ((unsigned long long)evict_key(now_worth) << 31) | unsigned(i));
+    }
   }
   mine = warp_min(mine);
   if (lane == 0) best[threadIdx.x >> 5] = mine;

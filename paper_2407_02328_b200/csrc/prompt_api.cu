@@ -60,6 +60,7 @@ adore_status_t packed_params(const adore_prompt_t* s, const int32_t* seq_start, 
   const adore_status_t st = check_heads(s->n_heads, s->n_kv_heads, s->head_dim, s->dtype, s->scale);
   if (st != ADORE_OK) return st;
   if (!aligned4({seq_start, err})) return ADORE_ERR_INVALID_ARG;
+  if (s->total > 0x7fff0000) return ADORE_ERR_UNSUPPORTED;      // row numbers plus a CTA's span stay within 31 bits
   p.seq_start = seq_start; p.S = s->n_seqs; p.total = s->total;
   p.H = s->n_heads; p.Hk = s->n_kv_heads; p.group = s->n_heads / s->n_kv_heads;
   p.scale = scale_of(s->scale, s->head_dim);
@@ -192,8 +193,10 @@ adore_status_t check_q4(const adore_q4_t* c) {
   if (!c || c->struct_size != sizeof(adore_q4_t) || c->batch < 1 || c->capacity < 1) return ADORE_ERR_INVALID_ARG;
   const adore_status_t st = check_heads(c->n_heads, c->n_kv_heads, c->head_dim, c->dtype, c->scale);
   if (st != ADORE_OK) return st;
-  // slot indices take 31 bits of a key, and every (sequence, head) is a CTA
-  if (c->capacity > (1 << 30) || int64_t(c->batch) * c->n_heads > kMaxGrid) return ADORE_ERR_UNSUPPORTED;
+  // slot indices take 31 bits of a key, every (sequence, head) is a CTA, and so are every 16 slots when a cache is filled
+  if (c->capacity > (1 << 30) || int64_t(c->batch) * c->n_heads > kMaxGrid ||
+      int64_t(c->batch) * c->n_kv_heads * (q4_padded(c->capacity) / 16) > kMaxGrid)
+    return ADORE_ERR_UNSUPPORTED;
   return ADORE_OK;
 }
 size_t q4_row_count(const adore_q4_t* c) { return size_t(c->batch) * c->n_kv_heads; }
@@ -203,9 +206,7 @@ adore_status_t pack_rows(const adore_q4_t* c, const PackedParams& p, const void*
                          const Q4Rows& rows, cudaStream_t st) {
   constexpr int kRows = 256 / (DH / 8);
   const int P = q4_padded(c->capacity);
-  const size_t R = q4_row_count(c);
-  if (R > 65535) return ADORE_ERR_UNSUPPORTED;
-  const dim3 grid(unsigned((P + kRows - 1) / kRows), unsigned(R));
+  const unsigned grid = unsigned(q4_row_count(c) * ((P + kRows - 1) / kRows));      // fits: check_q4
   evict_pack_kernel<T, DH><<<grid, 256, 0, st>>>(p, static_cast<const T*>(k), static_cast<const T*>(v), slot_pos, length, c->capacity, P, rows);
   return launched();
 }
@@ -340,8 +341,14 @@ adore_status_t adore_evict_prompt(const adore_q4_t* cache, const adore_prompt_t*
     return ADORE_ERR_INVALID_ARG;
   if (rows->total > 0 && (!acc || !k || !v || !aligned16({k, v}) || !aligned4({acc}))) return ADORE_ERR_INVALID_ARG;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  evict_select_kernel<<<unsigned(q4_row_count(cache)), kEvictThreads, 0, st>>>(seq_start, rows->total, cache->n_kv_heads, cache->capacity,
-                                                                               recent, acc, slot_pos, slot_acc, length, error_word);
+  // Rows of 1024 tokens on average take 256 threads (eight CTAs on an SM), longer ones 1024.
+  const unsigned rows_n = unsigned(q4_row_count(cache));
+  if (rows->total / rows->n_seqs <= 1024)
+    evict_select_kernel<256, 16><<<rows_n, 256, 0, st>>>(seq_start, rows->total, cache->n_kv_heads, cache->capacity, recent, acc, slot_pos,
+                                                         slot_acc, length, error_word);
+  else
+    evict_select_kernel<1024, 24><<<rows_n, 1024, 0, st>>>(seq_start, rows->total, cache->n_kv_heads, cache->capacity, recent, acc, slot_pos,
+                                                           slot_acc, length, error_word);
   s = launched();
   if (s != ADORE_OK) return s;
   const Q4Rows c = q4_rows(cache_rows, q4_row_count(cache), q4_padded(cache->capacity), cache->head_dim);

@@ -119,11 +119,21 @@ bool allow_smem(size_t bytes, bool wide = false) {
 
 template <typename T, int DH>
 adore_status_t attention_simt(const PackedParams& p, const void* q, const void* k, const void* v, void* out, float* lse, cudaStream_t st) {
-  const unsigned grid = tile_grid(p, kPsBlock, p.H);
-  if (grid == 0) return ADORE_ERR_UNSUPPORTED;
+  // Clusters of 4 (2) CTAs per tile while all tiles' CTAs together stay below about four (eight) on an SM: beyond that the tiles
+  // themselves keep the SMs busy, and the joins only cost.
+  const int64_t tiles = (int64_t(p.total) / kPsBlock + p.S) * p.H, sms = sm_count();
+  const int split = tiles <= 2 * sms ? 4 : tiles <= 4 * sms ? 2 : 1;
+  if (tiles * split > kMaxGrid) return ADORE_ERR_UNSUPPORTED;
   if (!allow_smem<prompt_attention_simt_kernel<T, DH>>(prompt_simt_smem<DH>())) return ADORE_ERR_CUDA;
-  prompt_attention_simt_kernel<T, DH><<<grid, kPsThreads, prompt_simt_smem<DH>(), st>>>(
-      p, static_cast<const T*>(q), static_cast<const T*>(k), static_cast<const T*>(v), static_cast<T*>(out), lse);
+  cudaLaunchConfig_t lc{};
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim.x = unsigned(split); at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
+  lc.gridDim = dim3(unsigned(tiles * split)); lc.blockDim = dim3(kPaThreads); lc.dynamicSmemBytes = prompt_simt_smem<DH>(); lc.stream = st;
+  lc.attrs = at; lc.numAttrs = split > 1 ? 1 : 0;
+  const cudaError_t e = cudaLaunchKernelEx(&lc, prompt_attention_simt_kernel<T, DH>, p, split, static_cast<const T*>(q),
+                                           static_cast<const T*>(k), static_cast<const T*>(v), static_cast<T*>(out), lse);
+  if (e != cudaSuccess) { cudaGetLastError(); return ADORE_ERR_CUDA; }
   return launched();
 }
 

@@ -3,18 +3,24 @@
 //   s_ij = scale q_i . k_j (j <= i),  lse_i = log sum_j exp s_ij,  out_i = sum_j exp(s_ij - lse_i) v_j
 //   acc_j = sum over a group's heads and the queries i >= j of exp(s_ij - lse_i)
 //
-// One CTA owns 64 query rows of one head (attention) or 64 key rows of one key/value head (weights) and walks over the
-// blocks of 64 rows on the other side. 256 threads as 16 x 16, 4 x 4 logits each: the tiles lie transposed in shared memory, so
-// that per element of the head dimension a thread reads two 16-byte pieces for 16 multiply-adds. Rows outside the sequence
-// are read as zeros and never stored.
+// Attention: 64 query rows of one head, shared by a cluster of 1, 2 or 4 CTAs that take every second or fourth block of 64 keys
+// (a tile's blocks are one after the other otherwise, and the last tiles of a long prompt set the time when there are few)
+// and join their maxima, sums and outputs through distributed shared memory. 128 threads as 8 x 16, 8 x 4 logits each.
+// Weights: 64 key rows of one key/value head, walking over the blocks of queries. 256 threads as 16 x 16, 4 x 4 logits each.
+// The tiles lie transposed in shared memory, so that per element of the head dimension a thread reads whole 16-byte pieces: 3 of
+// them for 32 multiply-adds, 2 for 16. (Attention with 4 x 4 logits was bound by those reads: 5 prompts of up to 1024 tokens,
+// 8 heads of 64: 132 us.) Rows outside the sequence are read as zeros and never stored.
 #pragma once
+
+#include <cooperative_groups.h>
 
 #include "packed.cuh"
 
 namespace adore {
 
 constexpr int kPsBlock = 64;
-constexpr int kPsThreads = 256;
+constexpr int kPsThreads = 256;            // weights
+constexpr int kPaThreads = 128;            // attention
 constexpr int kPsPitch = kPsBlock + 4;     // floats between the rows of a transposed tile
 
 template <int DH>
@@ -25,7 +31,7 @@ constexpr size_t prompt_weights_simt_smem() { return size_t(2 * DH * kPsPitch + 
 // 64 rows from `row0` of a sequence of `len` rows, transposed to dst[e][row]; lanes of a warp take 8 rows x 4 pieces.
 template <typename T, int DH>
 __device__ __forceinline__ void load_transposed(float* dst, const T* src, long long row_stride, int row0, int len) {
-  for (int i = threadIdx.x; i < kPsBlock * (DH / 4); i += kPsThreads) {
+  for (int i = threadIdx.x; i < kPsBlock * (DH / 4); i += blockDim.x) {
     const int low = i & 31, r = (low & 7) + 8 * ((i >> 5) & 7), c = (low >> 3) + 4 * (i >> 8);
     float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
     if (row0 + r < len) x = load4(src + (row0 + r) * row_stride + 4 * c);
@@ -34,82 +40,88 @@ __device__ __forceinline__ void load_transposed(float* dst, const T* src, long l
   }
 }
 
-// 4 x 4 logits of rows 4 ty.. of A against rows 4 tx.. of B, both transposed.
-template <int DH>
-__device__ __forceinline__ void tile_product(const float* a, const float* b, int ty, int tx, float (&s)[4][4]) {
+// R x 4 logits of rows R ty.. of A against rows 4 tx.. of B, both transposed.
+template <int DH, int R>
+__device__ __forceinline__ void tile_product(const float* a, const float* b, int ty, int tx, float (&s)[R][4]) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
+  for (int i = 0; i < R; ++i)
 #pragma unroll
     for (int j = 0; j < 4; ++j) s[i][j] = 0.f;
 #pragma unroll 8
   for (int e = 0; e < DH; ++e) {
-    const float4 x = *reinterpret_cast<const float4*>(a + e * kPsPitch + 4 * ty);
     const float4 y = *reinterpret_cast<const float4*>(b + e * kPsPitch + 4 * tx);
-    const float xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+    const float ys[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i0 = 0; i0 < R; i0 += 4) {
+      const float4 x = *reinterpret_cast<const float4*>(a + e * kPsPitch + R * ty + i0);
+      const float xs[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
-      for (int j = 0; j < 4; ++j) s[i][j] = fmaf(xs[i], ys[j], s[i][j]);
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s[i0 + i][j] = fmaf(xs[i], ys[j], s[i0 + i][j]);
+    }
   }
 }
 
 template <typename T, int DH>
-__global__ void __launch_bounds__(kPsThreads, 2) prompt_attention_simt_kernel(const PackedParams p, const T* q, const T* k,
-                                                                              const T* v, T* out, float* lse) {
+__global__ void __launch_bounds__(kPaThreads, DH == 64 ? 4 : 2) prompt_attention_simt_kernel(const PackedParams p, int split, const T* q,
+                                                                                            const T* k, const T* v, T* out, float* lse) {
   extern __shared__ __align__(16) float prompt_smem[];
   float* qt = prompt_smem;
   float* kt = qt + DH * kPsPitch;          // later the weights of the block, transposed
   float* vs = kt + DH * kPsPitch;
   __shared__ PackedTile tile;
   __shared__ int found;
-  const int h = blockIdx.x % p.H, g = h / p.group;
+  __shared__ float s_m[kPsBlock], s_l[kPsBlock];
+  const int rank = blockIdx.x % split, unit = blockIdx.x / split;
+  const int h = unit % p.H, g = h / p.group;
   if (threadIdx.x < 32) {
     PackedTile t{};
-    const bool ok = find_packed_tile<kPsBlock>(p.seq_start, p.S, p.total, blockIdx.x / p.H, p.err, t);
+    const bool ok = find_packed_tile<kPsBlock>(p.seq_start, p.S, p.total, unit / p.H, p.err, t);
     if (threadIdx.x == 0) { tile = t; found = ok; }
   }
   __syncthreads();
-  if (!found) return;
+  if (!found) return;                      // alike in all CTAs of the cluster
   const int len = tile.len, q0 = tile.index * kPsBlock;
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
   const T* qs = q + tile.start * p.q_row + h * p.q_head;
   const T* ks = k + tile.start * p.k_row + g * p.k_head;
   const T* vsrc = v + tile.start * p.v_row + g * p.v_head;
   load_transposed<T, DH>(qt, qs, p.q_row, q0, len);
-  constexpr int NV = DH / 64;              // 16-byte pieces of a value row per thread
-  float o[4][4 * NV], m[4], l[4];
+  constexpr int R = 8, NV = DH / 64;       // rows of a thread, 16-byte pieces of a value row per thread
+  float o[R][4 * NV], m[R], l[R];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    m[i] = -INFINITY;
+  for (int i = 0; i < R; ++i) {
+    m[i] = -1e30f;                         // finite: a CTA of the cluster may have no block, or only masked ones for a row
     l[i] = 0.f;
 #pragma unroll
     for (int j = 0; j < 4 * NV; ++j) o[i][j] = 0.f;
   }
   const float c = p.scale * 1.4426950408889634f;      // logits in units of log 2
-  for (int kb = 0; kb <= tile.index; ++kb) {
+  for (int kb = rank; kb <= tile.index; kb += split) {
     __syncthreads();
     load_transposed<T, DH>(kt, ks, p.k_row, kb * kPsBlock, len);
-    for (int i = threadIdx.x; i < kPsBlock * (DH / 4); i += kPsThreads) {
+    for (int i = threadIdx.x; i < kPsBlock * (DH / 4); i += kPaThreads) {
       const int r = i / (DH / 4), e = i % (DH / 4);
       float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
       if (kb * kPsBlock + r < len) x = load4(vsrc + (kb * kPsBlock + r) * p.v_row + 4 * e);
       *reinterpret_cast<float4*>(vs + r * DH + 4 * e) = x;
     }
     __syncthreads();
-    float s[4][4];
-    tile_product<DH>(qt, kt, ty, tx, s);
+    float s[R][4];
+    tile_product<DH, R>(qt, kt, ty, tx, s);
     const bool diagonal = kb == tile.index;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < R; ++i) {
       float top = -INFINITY;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        s[i][j] = diagonal && 4 * tx + j > 4 * ty + i ? -INFINITY : s[i][j] * c;
+        s[i][j] = diagonal && 4 * tx + j > R * ty + i ? -INFINITY : s[i][j] * c;
         top = fmaxf(top, s[i][j]);
       }
 #pragma unroll
       for (int w = 8; w > 0; w >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, w));
-      const float now = fmaxf(m[i], top), f = exp2f(m[i] - now);      // a row's own position is in its block: now is finite
+      const float now = fmaxf(m[i], top), f = exp2f(m[i] - now);
       m[i] = now;
       l[i] *= f;
 #pragma unroll
@@ -123,36 +135,78 @@ __global__ void __launch_bounds__(kPsThreads, 2) prompt_attention_simt_kernel(co
     __syncthreads();                       // every thread has read the key tile
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-      *reinterpret_cast<float4*>(kt + (4 * tx + j) * kPsPitch + 4 * ty) = make_float4(s[0][j], s[1][j], s[2][j], s[3][j]);
+#pragma unroll
+      for (int i = 0; i < R; i += 4)
+        *reinterpret_cast<float4*>(kt + (4 * tx + j) * kPsPitch + R * ty + i) = make_float4(s[i][j], s[i + 1][j], s[i + 2][j], s[i + 3][j]);
     __syncthreads();
 #pragma unroll 4
     for (int r = 0; r < kPsBlock; ++r) {
-      const float4 w = *reinterpret_cast<const float4*>(kt + r * kPsPitch + 4 * ty);
-      const float ws[4] = {w.x, w.y, w.z, w.w};
+      float ws[R];
+#pragma unroll
+      for (int i = 0; i < R; i += 4) {
+        const float4 w = *reinterpret_cast<const float4*>(kt + r * kPsPitch + R * ty + i);
+        ws[i] = w.x; ws[i + 1] = w.y; ws[i + 2] = w.z; ws[i + 3] = w.w;
+      }
 #pragma unroll
       for (int n = 0; n < NV; ++n) {
         const float4 x = *reinterpret_cast<const float4*>(vs + r * DH + 64 * n + 4 * tx);
         const float xs[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < R; ++i)
 #pragma unroll
           for (int j = 0; j < 4; ++j) o[i][4 * n + j] = fmaf(ws[i], xs[j], o[i][4 * n + j]);
       }
     }
   }
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
+  for (int i = 0; i < R; ++i)
 #pragma unroll
     for (int w = 8; w > 0; w >>= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], w);
-    const int r = q0 + 4 * ty + i;
-    if (r >= len) continue;
-    const float inv = 1.f / l[i];
-    T* dst = out + (tile.start + r) * p.out_row + h * p.out_head;
+  if (split == 1) {
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      const int r = q0 + R * ty + i;
+      if (r >= len) continue;
+      const float inv = 1.f / l[i];
+      T* dst = out + (tile.start + r) * p.out_row + h * p.out_head;
+#pragma unroll
+      for (int n = 0; n < NV; ++n)
+        store4(dst + 64 * n + 4 * tx, make_float4(o[i][4 * n] * inv, o[i][4 * n + 1] * inv, o[i][4 * n + 2] * inv, o[i][4 * n + 3] * inv));
+      if (lse != nullptr && tx == 0) lse[size_t(h) * p.total + tile.start + r] = m[i] * 0.6931471805599453f + logf(l[i]);
+    }
+    return;
+  }
+  // the cluster's parts: every CTA leaves its own in shared memory and joins 64 / split rows
+  namespace cg = cooperative_groups;
+  cg::cluster_group cluster = cg::this_cluster();
+  __syncthreads();
+  float* part = vs;                        // [64][DH]
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
 #pragma unroll
     for (int n = 0; n < NV; ++n)
-      store4(dst + 64 * n + 4 * tx, make_float4(o[i][4 * n] * inv, o[i][4 * n + 1] * inv, o[i][4 * n + 2] * inv, o[i][4 * n + 3] * inv));
-    if (lse != nullptr && tx == 0) lse[size_t(h) * p.total + tile.start + r] = m[i] * 0.6931471805599453f + logf(l[i]);
+      *reinterpret_cast<float4*>(part + (R * ty + i) * DH + 64 * n + 4 * tx) = make_float4(o[i][4 * n], o[i][4 * n + 1], o[i][4 * n + 2], o[i][4 * n + 3]);
+    if (tx == 0) { s_m[R * ty + i] = m[i]; s_l[R * ty + i] = l[i]; }
   }
+  cluster.sync();
+  const int rows = kPsBlock / split;
+  for (int i = threadIdx.x; i < rows * (DH / 4); i += kPaThreads) {
+    const int row = rank * rows + i / (DH / 4), e = 4 * (i % (DH / 4)), r = q0 + row;
+    if (r >= len) continue;
+    float top = -1e30f, sum = 0.f;
+    for (int x = 0; x < split; ++x) top = fmaxf(top, *cluster.map_shared_rank(&s_m[row], x));
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int x = 0; x < split; ++x) {
+      const float f = exp2f(*cluster.map_shared_rank(&s_m[row], x) - top);
+      const float4 y = *reinterpret_cast<const float4*>(cluster.map_shared_rank(part + row * DH + e, x));
+      sum = fmaf(f, *cluster.map_shared_rank(&s_l[row], x), sum);
+      acc.x = fmaf(f, y.x, acc.x); acc.y = fmaf(f, y.y, acc.y); acc.z = fmaf(f, y.z, acc.z); acc.w = fmaf(f, y.w, acc.w);
+    }
+    const float inv = 1.f / sum;
+    store4(out + (tile.start + r) * p.out_row + h * p.out_head + e, make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv));
+    if (lse != nullptr && e == 0) lse[size_t(h) * p.total + tile.start + r] = top * 0.6931471805599453f + logf(sum);
+  }
+  cluster.sync();                          // nobody leaves while its shared memory is read
 }
 
 template <typename T, int DH>
@@ -191,7 +245,7 @@ __global__ void __launch_bounds__(kPsThreads, 2) prompt_weights_simt_kernel(cons
       }
       __syncthreads();
       float s[4][4];
-      tile_product<DH>(kt, qt, ty, tx, s);
+      tile_product<DH, 4>(kt, qt, ty, tx, s);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         float part = 0.f;

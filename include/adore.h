@@ -468,6 +468,7 @@ size_t adore_q4_bytes(const adore_q4_t *shape);
  *   acc: float[n_kv_heads, rows->total].  cache_rows: the buffer, written whole.
  *   slot_pos: out.  slot_acc: out, float[batch, n_kv_heads, C], acc of the kept tokens, 0 in empty slots.
  *   length: out, int32[batch, n_kv_heads], tokens of the sequence (0 for a sequence that is skipped).
+ * batch and n_kv_heads are at most 65535 here (UNSUPPORTED).
  * Errors: INVALID_ARG, UNSUPPORTED, CUDA. */
 adore_status_t adore_evict_prompt(const adore_q4_t *cache, const adore_prompt_t *rows, const int32_t *seq_start,
                                   const float *acc, const void *k, const void *v, int32_t recent, void *cache_rows,
@@ -500,7 +501,7 @@ adore_status_t adore_q4_attention(const adore_q4_t *cache, const void *q, const 
 
 /* The values that cache rows stand for: k_out, v_out T[batch, n_kv_heads, n, dh] of slots slots[b, g, i] (int32; outside
  * [0, C): zeros), or of all slots in order when slots is NULL (n = C). For checking, and for moving rows back to a cache
- * in full precision (Section 2.1's rows). Errors: INVALID_ARG, UNSUPPORTED, CUDA. */
+ * in full precision (Section 2.1's rows). Errors: INVALID_ARG, UNSUPPORTED (batch or n_kv_heads above 65535), CUDA. */
 adore_status_t adore_q4_read(const adore_q4_t *cache, const void *cache_rows, const int32_t *slots, int32_t n,
                              void *k_out, void *v_out, void *cuda_stream);
 

@@ -419,16 +419,23 @@ def adore_prompt_weights(q, k, lse, seq_start, acc, window: int = 0, scale: floa
                                        _at(error_word), _stream(cuda_stream, device)), where)
 
 
-def _q4(where: str, like, batch: int, n_heads: int, n_kv_heads: int, head_dim: int, capacity: int, cache, scale: float = 0.0):
-    """The shape of a cache (heads, dtype as `like`'s), and its device; the buffer has to be large enough."""
-    c = adore_q4_t(C.sizeof(adore_q4_t), _elem(where, like), batch, n_heads, n_kv_heads, head_dim, capacity, scale)
-    device = like.get_device()
-    _tensors(where, device, (("cache", cache, _torch().uint8, cache.shape),))
-    _device(where, "cache", cache)
-    need = _lib().adore_q4_bytes(C.byref(c))
-    if cache.numel() < need:
-        _refuse(where, f"the cache has {cache.numel()} bytes, {need} are needed")
-    return c, device
+_Q4_SHAPES: Dict[tuple, tuple] = {}     # (dtype, sizes, scale) -> (adore_q4_t by reference, bytes of its buffer)
+
+
+def _q4(where: str, like, sizes: tuple, cache, scale: float = 0.0):
+    """The shape of a cache (sizes: batch, heads, kv_heads, head_dim, capacity; element type as `like`'s) and its device; the
+    buffer has to be large enough."""
+    known = _Q4_SHAPES.get((like.dtype, sizes, scale))
+    if known is None:
+        c = adore_q4_t(C.sizeof(adore_q4_t), _elem(where, like), *sizes, scale)
+        known = C.byref(c), _lib().adore_q4_bytes(C.byref(c))
+        if len(_Q4_SHAPES) > 512:
+            _Q4_SHAPES.clear()
+        _Q4_SHAPES[like.dtype, sizes, scale] = known
+    device = _device(where, "cache", cache)
+    if cache.dtype is not _torch().uint8 or not cache.is_contiguous() or cache.numel() < known[1]:
+        _refuse(where, f"the cache is {cache.dtype} [{cache.numel()}], uint8 [{known[1]}] is needed")
+    return known[0], device
 
 
 def adore_q4_bytes(batch: int, n_kv_heads: int, head_dim: int, capacity: int) -> int:
@@ -448,11 +455,11 @@ def adore_evict_prompt(acc, k, v, seq_start, recent: int, cache, slot_pos, slot_
     if slot_pos.dim() != 3:
         _refuse(where, "slot_pos is int32 [sequences, kv_heads, capacity]")
     shape = (p.n_seqs, p.n_kv_heads, slot_pos.shape[2])
-    c, _ = _q4(where, k, p.n_seqs, p.n_heads, p.n_kv_heads, p.head_dim, shape[2], cache)
+    c, _ = _q4(where, k, (p.n_seqs, p.n_heads, p.n_kv_heads, p.head_dim, shape[2]), cache)
     _tensors(where, device, (("acc", acc, torch.float32, (p.n_kv_heads, p.total)), ("slot_pos", slot_pos, torch.int32, shape),
                              ("slot_acc", slot_acc, torch.float32, shape), ("length", length, torch.int32, shape[:2]),
                              ("error_word", error_word, torch.int32, (1,))))
-    _check(_lib().adore_evict_prompt(C.byref(c), C.byref(p), seq_start.data_ptr(), acc.data_ptr(), k.data_ptr(), v.data_ptr(), recent,
+    _check(_lib().adore_evict_prompt(c, C.byref(p), seq_start.data_ptr(), acc.data_ptr(), k.data_ptr(), v.data_ptr(), recent,
                                      cache.data_ptr(), slot_pos.data_ptr(), slot_acc.data_ptr(), length.data_ptr(), _at(error_word),
                                      _stream(cuda_stream, device)), where)
 
@@ -465,13 +472,13 @@ def adore_evict_step(weights, k_new, v_new, recent: int, cache, slot_pos, slot_a
     if weights.dim() != 3 or k_new.dim() != 3 or slot_pos.dim() != 3:
         _refuse(where, "weights [batch, heads, capacity + 1], k_new [batch, kv_heads, dh], slot_pos [batch, kv_heads, capacity]")
     (b, hk, dh), h, cap, i32, f32, dtype = k_new.shape, weights.shape[1], slot_pos.shape[2], torch.int32, torch.float32, k_new.dtype
-    c, device = _q4(where, k_new, b, h, hk, dh, cap, cache)
+    c, device = _q4(where, k_new, (b, h, hk, dh, cap), cache)
     slots, heads, rows = (b, hk, cap), (b, hk), (b, hk, dh)
     _tensors(where, device, (("weights", weights, f32, (b, h, cap + 1)), ("k_new", k_new, dtype, rows), ("v_new", v_new, dtype, rows),
                              ("slot_pos", slot_pos, i32, slots), ("slot_acc", slot_acc, f32, slots), ("length", length, i32, heads),
                              ("admit_slot", admit_slot, i32, heads), ("evicted_pos", evicted_pos, i32, heads),
                              ("error_word", error_word, i32, (1,))))
-    _check(_lib().adore_evict_step(C.byref(c), weights.data_ptr(), k_new.data_ptr(), v_new.data_ptr(), recent, cache.data_ptr(),
+    _check(_lib().adore_evict_step(c, weights.data_ptr(), k_new.data_ptr(), v_new.data_ptr(), recent, cache.data_ptr(),
                                    slot_pos.data_ptr(), slot_acc.data_ptr(), length.data_ptr(), admit_slot.data_ptr(), evicted_pos.data_ptr(),
                                    _at(error_word), _stream(cuda_stream, device)), where)
 
@@ -483,11 +490,11 @@ def adore_q4_attention(q, k_new, v_new, cache, slot_pos, out, weights=None, scal
     if q.dim() != 3 or slot_pos.dim() != 3:
         _refuse(where, "q [batch, heads, dh], slot_pos [batch, kv_heads, capacity]")
     (b, h, dh), (_, hk, cap), dtype = q.shape, slot_pos.shape, q.dtype
-    c, device = _q4(where, q, b, h, hk, dh, cap, cache, scale)
+    c, device = _q4(where, q, (b, h, hk, dh, cap), cache, scale)
     _tensors(where, device, (("q", q, dtype, (b, h, dh)), ("k_new", k_new, dtype, (b, hk, dh)), ("v_new", v_new, dtype, (b, hk, dh)),
                              ("slot_pos", slot_pos, torch.int32, (b, hk, cap)), ("out", out, dtype, (b, h, dh)),
                              ("weights", weights, torch.float32, (b, h, cap + 1))))
-    _check(_lib().adore_q4_attention(C.byref(c), q.data_ptr(), _at(k_new), _at(v_new), cache.data_ptr(), slot_pos.data_ptr(), out.data_ptr(),
+    _check(_lib().adore_q4_attention(c, q.data_ptr(), _at(k_new), _at(v_new), cache.data_ptr(), slot_pos.data_ptr(), out.data_ptr(),
                                      _at(weights), _stream(cuda_stream, device)), where)
 
 
@@ -498,11 +505,11 @@ def adore_q4_read(cache, capacity: int, slots, k_out, v_out, cuda_stream=None) -
     if k_out.dim() != 4:
         _refuse(where, "k_out [batch, kv_heads, n, dh]")
     b, hk, n, dh = shape = k_out.shape
-    c, device = _q4(where, k_out, b, hk, hk, dh, capacity, cache)
+    c, device = _q4(where, k_out, (b, hk, hk, dh, capacity), cache)
     listed = (b, hk) if slots is not None and n == 1 and slots.dim() == 2 else (b, hk, n)
     _tensors(where, device, (("slots", slots, _torch().int32, listed), ("k_out", k_out, k_out.dtype, shape),
                              ("v_out", v_out, k_out.dtype, shape)))
-    _check(_lib().adore_q4_read(C.byref(c), cache.data_ptr(), _at(slots), n, k_out.data_ptr(), v_out.data_ptr(),
+    _check(_lib().adore_q4_read(c, cache.data_ptr(), _at(slots), n, k_out.data_ptr(), v_out.data_ptr(),
                                 _stream(cuda_stream, device)), where)
 
 

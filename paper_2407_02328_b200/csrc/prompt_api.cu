@@ -119,10 +119,11 @@ bool allow_smem(size_t bytes, bool wide = false) {
 
 template <typename T, int DH>
 adore_status_t attention_simt(const PackedParams& p, const void* q, const void* k, const void* v, void* out, float* lse, cudaStream_t st) {
-  // Clusters of 4 (2) CTAs per tile while all tiles' CTAs together stay below about four (eight) on an SM: beyond that the tiles
-  // themselves keep the SMs busy, and the joins only cost.
-  const int64_t tiles = (int64_t(p.total) / kPsBlock + p.S) * p.H, sms = sm_count();
-  const int split = tiles <= 2 * sms ? 4 : tiles <= 4 * sms ? 2 : 1;
+  // Clusters of 4 (2) CTAs per tile while half (all) of the tiles' single CTAs are resident at once; beyond that the tiles
+  // themselves keep the SMs busy and the joins only cost. 8 heads of 64, one prompt of 1024: 1, 2, 4 CTAs 105, 72, 55 us;
+  // 16 heads of 64, 8 prompts of 1024: 519, 570, 665 us.
+  const int64_t tiles = (int64_t(p.total) / kPsBlock + p.S) * p.H, resident = int64_t(sm_count()) * (DH == 64 ? 4 : 2);
+  const int split = 2 * tiles <= resident ? 4 : tiles <= resident ? 2 : 1;
   if (tiles * split > kMaxGrid) return ADORE_ERR_UNSUPPORTED;
   if (!allow_smem<prompt_attention_simt_kernel<T, DH>>(prompt_simt_smem<DH>())) return ADORE_ERR_CUDA;
   cudaLaunchConfig_t lc{};
@@ -203,10 +204,8 @@ adore_status_t check_q4(const adore_q4_t* c) {
   if (!c || c->struct_size != sizeof(adore_q4_t) || c->batch < 1 || c->capacity < 1) return ADORE_ERR_INVALID_ARG;
   const adore_status_t st = check_heads(c->n_heads, c->n_kv_heads, c->head_dim, c->dtype, c->scale);
   if (st != ADORE_OK) return st;
-  // slot indices take 31 bits of a key, every (sequence, head) is a CTA, and so are every 16 slots when a cache is filled
-  if (c->capacity > (1 << 30) || int64_t(c->batch) * c->n_heads > kMaxGrid ||
-      int64_t(c->batch) * c->n_kv_heads * (q4_padded(c->capacity) / 16) > kMaxGrid)
-    return ADORE_ERR_UNSUPPORTED;
+  // slot indices take 31 bits of a key, and every (sequence, head) is a CTA
+  if (c->capacity > (1 << 30) || int64_t(c->batch) * c->n_heads > kMaxGrid) return ADORE_ERR_UNSUPPORTED;
   return ADORE_OK;
 }
 size_t q4_row_count(const adore_q4_t* c) { return size_t(c->batch) * c->n_kv_heads; }
@@ -216,7 +215,7 @@ adore_status_t pack_rows(const adore_q4_t* c, const PackedParams& p, const void*
                          const Q4Rows& rows, cudaStream_t st) {
   constexpr int kRows = 256 / (DH / 8);
   const int P = q4_padded(c->capacity);
-  const unsigned grid = unsigned(q4_row_count(c) * ((P + kRows - 1) / kRows));      // fits: check_q4
+  const dim3 grid(unsigned((P + kRows - 1) / kRows), unsigned(c->n_kv_heads), unsigned(c->batch));
   evict_pack_kernel<T, DH><<<grid, 256, 0, st>>>(p, static_cast<const T*>(k), static_cast<const T*>(v), slot_pos, length, c->capacity, P, rows);
   return launched();
 }
@@ -285,10 +284,9 @@ adore_status_t attend_q4(const adore_q4_t* c, const void* q, const void* k, cons
 
 template <typename T, int DH>
 adore_status_t read_rows(const adore_q4_t* c, const Q4Rows& rows, const int* slots, int n, void* k, void* v, cudaStream_t st) {
-  const size_t pieces = q4_row_count(c) * n * (DH / 8);
-  const unsigned grid = unsigned(std::min<size_t>((pieces + 255) / 256, 148 * 64));
-  q4_read_kernel<T, DH><<<grid, 256, 0, st>>>(rows, q4_padded(c->capacity), c->capacity, slots, n, pieces, static_cast<T*>(k),
-                                              static_cast<T*>(v));
+  constexpr int kRows = 256 / (DH / 8);
+  const dim3 grid(unsigned((int64_t(n) + kRows - 1) / kRows), unsigned(c->n_kv_heads), unsigned(c->batch));
+  q4_read_kernel<T, DH><<<grid, 256, 0, st>>>(rows, q4_padded(c->capacity), c->capacity, slots, n, static_cast<T*>(k), static_cast<T*>(v));
   return launched();
 }
 
@@ -347,6 +345,7 @@ adore_status_t adore_evict_prompt(const adore_q4_t* cache, const adore_prompt_t*
   if (rows->n_seqs != cache->batch || rows->n_heads != cache->n_heads || rows->n_kv_heads != cache->n_kv_heads ||
       rows->head_dim != cache->head_dim || rows->dtype != cache->dtype || recent < 1 || recent > cache->capacity)
     return ADORE_ERR_INVALID_ARG;
+  if (cache->batch > 65535 || cache->n_kv_heads > 65535) return ADORE_ERR_UNSUPPORTED;      // grid dimensions
   if (!cache_rows || !slot_pos || !slot_acc || !length || !aligned16({cache_rows}) || !aligned4({slot_pos, slot_acc, length}))
     return ADORE_ERR_INVALID_ARG;
   if (rows->total > 0 && (!acc || !k || !v || !aligned16({k, v}) || !aligned4({acc}))) return ADORE_ERR_INVALID_ARG;
@@ -398,6 +397,7 @@ adore_status_t adore_q4_read(const adore_q4_t* cache, const void* cache_rows, co
   if (s != ADORE_OK) return s;
   if (n < 0 || (slots == nullptr && n != cache->capacity) || !cache_rows || !aligned16({cache_rows, k_out, v_out}) || !aligned4({slots}))
     return ADORE_ERR_INVALID_ARG;
+  if (cache->batch > 65535 || cache->n_kv_heads > 65535) return ADORE_ERR_UNSUPPORTED;      // grid dimensions
   if (n == 0) return ADORE_OK;
   if (!k_out || !v_out) return ADORE_ERR_INVALID_ARG;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);

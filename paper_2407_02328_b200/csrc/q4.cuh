@@ -86,15 +86,16 @@ __device__ __forceinline__ uint32_t q4_encode8(const float (&x)[8], __nv_bfloat1
   uint32_t w = 0;
   if (stepf > 1e-35f && stepf < 1e35f) {
     const uint32_t half = __float_as_uint(0.5f * stepf);
+    const float most = 15.f * stepf;
     constexpr uint32_t kRound = 0x4b400000u;                   // 1.5 * 2^23: the low bits of t + that are t rounded
 #pragma unroll
     for (int i = 7; i >= 0; --i) {
-      const float d = x[i] - lowf, t = fminf(fmaxf(d * inv, 0.f), 15.f);
+      const float d = fminf(fmaxf(x[i] - lowf, 0.f), most), t = d * inv;      // (clamped first: 15 step is exact)
       float u = t + __uint_as_float(kRound);
       const float rest = fmaf(-(u - __uint_as_float(kRound)), stepf, d);
       const bool off = fabsf(rest) > __uint_as_float(half - (__float_as_uint(u) & 1u));
       const float to = u + __uint_as_float((__float_as_uint(rest) & 0x80000000u) | 0x3f800000u);
-      u = off && t > 0.f && t < 15.f ? to : u;                 // clamped values stay
+      u = off ? to : u;
       w = w * 16u + __float_as_uint(u);
     }
     w -= kRound * 0x11111111u;                                 // what the words beside the codes added up to
@@ -131,14 +132,15 @@ __device__ __forceinline__ void q4_store_piece(const Q4Rows& c, size_t r, int P,
   }
 }
 
-// Rows back to T: one thread per 8 elements of a listed row.
+// Rows back to T: one thread per 8 elements of a listed row; grid (rows, key/value heads, batch).
 template <typename T, int DH>
-__global__ void __launch_bounds__(256) q4_read_kernel(const Q4Rows c, int P, int C, const int* slots, int n, size_t pieces,
-                                                      T* k_out, T* v_out) {
-  for (size_t i = blockIdx.x * size_t(blockDim.x) + threadIdx.x; i < pieces; i += size_t(gridDim.x) * blockDim.x) {
-    const int j = int(i % (DH / 8));
-    const size_t row = i / (DH / 8), r = row / n;
-    const int slot = slots != nullptr ? slots[row] : int(row % n);
+__global__ void __launch_bounds__(256) q4_read_kernel(const Q4Rows c, int P, int C, const int* slots, int n, T* k_out, T* v_out) {
+  constexpr int LPR = DH / 8, ROWS = 256 / LPR;
+  const size_t r = size_t(blockIdx.z) * gridDim.y + blockIdx.y;
+  const int i = blockIdx.x * ROWS + threadIdx.x / LPR, j = threadIdx.x % LPR;
+  if (i < n) {
+    const size_t row = r * n + i;
+    const int slot = slots != nullptr ? slots[row] : i;
     float kx[8], vx[8];
     if (slot >= 0 && slot < C) {
       const uint32_t kw = c.k[(r * P + slot) * (DH / 8) + q4_k_word<DH>(j)];

@@ -13,8 +13,10 @@
 //           exact; three if float, 24 bits), scaled by a power of two per head.
 //   values: A = codes of 16 elements x 16 slots as 128 + code (one AND-OR), B = weight x step of the slot as bfloat16
 //           (T bfloat16: rounded, half a step 2^-8, as the output is; float: three terms), brought from the logits' layout to
-//           B's by movmatrix. The excess 128 sum B comes from one more product with ones; float subtracts the 128 first,
-//           because the difference of the two sums would cost it 4 bits.
+//           B's by movmatrix. The excess 136 sum B comes from one more product with ones: what the rounding of B acts on is
+//           code - 8 then, between -8 and 7, with 8 step added to low (rounding against codes of 0 to 15 made the
+//           output's error 1.6 times that of its own rounding, 1.4 so). Float subtracts 128 first, because the difference of
+//           the two sums would cost it 4 bits.
 // A CTA is 4 or 8 warps, each with its own chunks of 16 slots, its own ring of shared-memory stages (cp.async, no barrier between
 // warps), running maximum, sum and accumulators. Warps are joined through shared memory, the CTAs that share a (sequence,
 // key/value head, block of 16 query heads) through a cluster's distributed shared memory: one launch, no workspace. The
@@ -374,7 +376,7 @@ q4_attention_kernel(const Q4Rows c, int H, int Hk, int C, int P, int blocks, int
       for (int y = 0; y < NB; ++y)
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-          const float st = q4_low_half(pair[u][n]), lo = q4_high_half(pair[u][n]);
+          const float st = q4_low_half(pair[u][n]), lo = fmaf(TERMS == 1 ? 8.f : 0.f, st, q4_high_half(pair[u][n]));
           uint32_t t[TERMS];
           q4_terms<TERMS>(x[y][u][0] * st, x[y][u][1] * st, t);
 #pragma unroll
@@ -420,7 +422,7 @@ q4_attention_kernel(const Q4Rows c, int H, int Hk, int C, int P, int blocks, int
         s_m[warp][h] = m[y][e];
         s_l[warp][h] = l[y][e];
 #pragma unroll
-        for (int n = 0; n < NG; ++n) s_low[warp][h][n] = low_acc[y][e][n] - 128.f * excess[y][n][e];
+        for (int n = 0; n < NG; ++n) s_low[warp][h][n] = low_acc[y][e][n] - 136.f * excess[y][n][e];
       }
     }
   __syncthreads();                            // every warp is done with its ring
@@ -487,9 +489,21 @@ q4_attention_kernel(const Q4Rows c, int H, int Hk, int C, int P, int blocks, int
     for (int h = 0; h < nh; ++h) {
       float* row = weights + (h0 + h) * (size_t(C) + 1);
       const float top = s_top[h], inv = s_inv[h];
-      for (int chunk = rank * WARPS; chunk < chunks; chunk += step) {
-        const int s = chunk * kQ4Chunk + threadIdx.x;
-        if (threadIdx.x < WARPS * kQ4Chunk && s < C) row[s] = q4_exp2(row[s] - top) * inv;
+      // slots in runs of 16 WARPS, every ctas-th run; four of a thread's loads in flight
+      constexpr int kRun = WARPS * kQ4Chunk, U = 4;
+      const int runs = (C + kRun - 1) / kRun, mine = (runs - rank + ctas - 1) / ctas * kRun;
+      for (int i0 = threadIdx.x; i0 < mine; i0 += 32 * WARPS * U) {
+        float x[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const int i = i0 + 32 * WARPS * u, s = (i / kRun * ctas + rank) * kRun + i % kRun;
+          x[u] = i < mine && s < C ? row[s] : 0.f;
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const int i = i0 + 32 * WARPS * u, s = (i / kRun * ctas + rank) * kRun + i % kRun;
+          if (i < mine && s < C) row[s] = q4_exp2(x[u] - top) * inv;
+        }
       }
       if (rank == 0 && threadIdx.x == 0) row[C] = s_l[0][h] * inv;
     }

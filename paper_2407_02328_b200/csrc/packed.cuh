@@ -32,7 +32,8 @@ __device__ __forceinline__ int packed_len(const int* seq_start, int s, int total
 
 // The tile of BLOCK rows with the given rank, tiles counted from the highest index within their sequence down (all last
 // tiles of the longest sequences first). Under a causal mask the work of a tile grows with its index, so a launch whose
-// CTAs take their rank from blockIdx starts the longest ones first and ends evenly. One warp calls it; no table and no
+// CTAs take their rank from blockIdx starts the longest ones first and ends evenly. (Sequence by sequence, so that the
+// tiles at work share their keys in L2, ended up to 10 % later: less even.) One warp calls it; no table and no
 // workspace is needed: the number of tiles with an index >= p is a sum over the sequences, p is found by bisection.
 // Returns false if there are fewer tiles.
 template <int BLOCK>

@@ -105,6 +105,56 @@ def test_scales_and_peaked_rows(dtype):
     _check([300], dtype=dtype, q_scale=1e-3)                  # all weights alike
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_more_tiles_than_ctas(dtype):
+    _check([200, 130, 300, 1, 64] * 12, h=8, hk=4, dh=64, dtype=dtype, window=90)          # several tiles per persistent CTA
+    _check([270, 120] * 12, h=8, hk=8, dh=128, dtype=dtype, pad=9)
+
+
+def test_empty_batches_and_empty_sequences():
+    import torch
+    from paper_2407_02328_b200 import adore as lib
+    for total in (0, 5):
+        q, k = torch.zeros(total, 4, 64, device="cuda").bfloat16(), torch.zeros(total, 2, 64, device="cuda").bfloat16()
+        out, lse, acc = torch.full_like(q, 7.0), torch.full((4, total), 7.0, device="cuda"), torch.full((2, total), 7.0, device="cuda")
+        start = torch.zeros(4, dtype=torch.int32, device="cuda")
+        word = torch.zeros(1, dtype=torch.int32, device="cuda")
+        lib.adore_prompt_attention(q, k, k, start, out, lse, error_word=word)
+        lib.adore_prompt_weights(q, k, lse, start, acc, error_word=word)
+        assert (out == 7).all() and (lse == 7).all() and (acc == 7).all() and word.item() == 0
+
+
+def test_two_streams_at_once():
+    import torch
+    from paper_2407_02328_b200 import adore as lib
+    lens = [900, 300, 77]
+    start, sets = _seq(lens), []
+    for seed in range(3):
+        q, k, v = _inputs(lens, 8, 2, 128, "bf16", seed)
+        sets.append((q, k, v, torch.zeros_like(q), torch.zeros(8, sum(lens), device="cuda"), torch.zeros(2, sum(lens), device="cuda")))
+
+    def run(q, k, v, out, lse, acc):
+        lib.adore_prompt_attention(q, k, v, start, out, lse)
+        lib.adore_prompt_weights(q, k, lse, start, acc)
+
+    alone = []
+    for s in sets:
+        run(*s)
+        alone.append([x.clone() for x in s[3:]])
+        for x in s[3:]:
+            x.zero_()
+    streams = [torch.cuda.Stream() for _ in sets]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for st, s in zip(streams, sets):
+            with torch.cuda.stream(st):
+                run(*s)
+    torch.cuda.synchronize()
+    for s, a in zip(sets, alone):
+        for x, y in zip(s[3:], a):
+            assert torch.equal(x, y)
+
+
 def test_long_prompt_bf16():
     _check([2500, 1, 611], h=4, hk=1, dh=128, window=32)
 

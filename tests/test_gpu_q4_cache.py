@@ -143,6 +143,36 @@ def test_rows_in_four_bits(dtype, dh):
     assert (kp[:, :, 1:3] == 0).all() and (vp[:, :, 1:3] == 0).all()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dh", [64, 128])
+def test_codes_of_rows_full_of_ties_and_of_every_size(dtype, dh):
+    """Quotients that are exactly halves of a step, rows of small whole numbers, and magnitudes from subnormal to huge."""
+    import torch
+    from paper_2407_02328_b200 import adore as lib
+    from tests import prompt_reference as ref
+    g = torch.Generator().manual_seed(dh)
+    n, kinds = 400, []
+    kinds.append(torch.randint(-20, 21, (n, 1, dh), generator=g).float())                      # short differences
+    base = torch.randint(0, 31, (n, 1, dh), generator=g).float() / 2                           # halves of a step of 1
+    base[:, :, ::64], base[:, :, 1::64] = 0.0, 15.0
+    kinds.append(base * torch.exp2(torch.randint(-60, 60, (n, 1, 1), generator=g).float()))
+    kinds.append(torch.randn(n, 1, dh, generator=g) * torch.exp2(torch.randint(-149, 120, (n, 1, 1), generator=g).float()))
+    kinds.append(torch.randn(n, 1, dh, generator=g) + 300 * torch.randn(n, 1, 1, generator=g))  # a small range far from zero
+    near = base + torch.exp2(torch.randint(-24, -10, (n, 1, dh), generator=g).float()) * torch.sign(torch.randn(n, 1, dh, generator=g))
+    kinds.append(near)                                                                         # next to halves
+    rows = torch.cat(kinds).to(_dt(dtype)).cuda()
+    c = rows.shape[0]
+    start = torch.tensor([0, c], dtype=torch.int32, device="cuda")
+    cache = torch.zeros(lib.adore_q4_bytes(1, 1, dh, c), dtype=torch.uint8, device="cuda")
+    pos, acc = torch.zeros(1, 1, c, dtype=torch.int32, device="cuda"), torch.zeros(1, 1, c, device="cuda")
+    length = torch.zeros(1, 1, dtype=torch.int32, device="cuda")
+    lib.adore_evict_prompt(torch.ones(1, c, device="cuda"), rows, rows.flip(0).contiguous(), start, 1, cache, pos, acc, length)
+    k, v = (torch.zeros(1, 1, c, dh, dtype=_dt(dtype), device="cuda") for _ in range(2))
+    lib.adore_q4_read(cache, c, None, k, v)
+    want = ref.in_four_bits(rows.cpu()[:, 0])[0].to(_dt(dtype))
+    assert torch.equal(k.cpu()[0, 0], want) and torch.equal(v.cpu()[0, 0], want.flip(0))
+
+
 def _evict_prompt(lens, hk, dh, dtype, c, recent, acc, seed=1, pad=0, fused=False):
     import torch
     from paper_2407_02328_b200 import adore as lib
@@ -214,6 +244,27 @@ def test_evict_prompt_long_rows():
     acc = torch.exp(2 * torch.randn(2, 70001, generator=g, device="cuda"))
     _evict_prompt([70001], 2, 64, "bf16", 1000, 100, acc)
     _evict_prompt([60000, 10001], 2, 64, "bf16", 20001, 1, acc)
+
+
+def test_evict_prompt_one_long_row_among_short_ones():
+    import torch
+    lens = [6000] + [3, 50] * 6                                       # the average picks the variant for short rows
+    g = torch.Generator("cuda").manual_seed(6)
+    acc = torch.randint(0, 300, (2, sum(lens)), generator=g, device="cuda").float()
+    _evict_prompt(lens, 2, 64, "bf16", 40, 7, acc)
+    _evict_prompt(lens, 2, 64, "f32", 5000, 1, acc)
+
+
+def test_evict_prompt_with_no_tokens():
+    import torch
+    from paper_2407_02328_b200 import adore as lib
+    for total in (0, 6):
+        k, acc = torch.zeros(total, 2, 64, device="cuda").bfloat16(), torch.zeros(2, total, device="cuda")
+        cache = torch.full((lib.adore_q4_bytes(3, 2, 64, 20),), 255, dtype=torch.uint8, device="cuda")
+        pos, val = torch.zeros(3, 2, 20, dtype=torch.int32, device="cuda"), torch.ones(3, 2, 20, device="cuda")
+        length = torch.ones(3, 2, dtype=torch.int32, device="cuda")
+        lib.adore_evict_prompt(acc, k, k, torch.zeros(4, dtype=torch.int32, device="cuda"), 5, cache, pos, val, length)
+        assert (pos == -1).all() and (val == 0).all() and (length == 0).all() and (cache == 0).all()
 
 
 def test_evict_prompt_skips_bad_sequences():
@@ -295,6 +346,40 @@ def test_evict_step_ties_odd_values_and_nothing_to_release():
         assert torch.equal(admit.cpu(), r_admit) and torch.equal(evicted.cpu(), r_evicted)
         assert torch.equal(pos.cpu(), state[0]) and torch.equal(val.cpu().nan_to_num(nan=-7.0), state[1].nan_to_num(nan=-7.0))
         assert length.flatten().tolist() == [61, 61] and word.item() == (4 if kind == 3 else 0)
+
+
+def test_decode_across_a_cluster_captured_and_on_two_streams():
+    """Long caches are shared by a cluster of CTAs: the same bits from a graph and with another call beside it."""
+    import torch
+    from paper_2407_02328_b200 import adore as lib
+    b, h, hk, c, dh = 2, 8, 2, 9001, 128
+    sets = []
+    for seed in (1, 2):
+        cache, pos, _, _ = _random_cache(b, hk, c, dh, "bf16", seed, 0.9)
+        q, kn, vn = (torch.randn(b, n, dh, device="cuda").bfloat16() for n in (h, hk, hk))
+        sets.append((q, kn, vn, cache, pos, torch.zeros_like(q), torch.zeros(b, h, c + 1, device="cuda")))
+    alone = []
+    for s in sets:
+        lib.adore_q4_attention(*s)
+        alone.append((s[5].clone(), s[6].clone()))
+    streams = [torch.cuda.Stream() for _ in sets]
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for st, s in zip(streams, sets):
+            with torch.cuda.stream(st):
+                lib.adore_q4_attention(*s)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        for s in sets:
+            lib.adore_q4_attention(*s)
+    for s, a in zip(sets, alone):
+        assert torch.equal(s[5], a[0]) and torch.equal(s[6], a[1])
+        s[5].zero_()
+        s[6].zero_()
+    graph.replay()
+    for s, a in zip(sets, alone):
+        assert torch.equal(s[5], a[0]) and torch.equal(s[6], a[1])
 
 
 @pytest.mark.parametrize("dtype,h,hk,dh", [("bf16", 8, 2, 128), ("f32", 4, 4, 64)])

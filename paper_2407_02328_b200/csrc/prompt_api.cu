@@ -229,18 +229,21 @@ adore_status_t step_rows(const adore_q4_t* c, const float* weights, const void* 
   return launched();
 }
 
-// Warps of a CTA (4 or 8) and CTAs that share a (sequence, key/value head, head block; 1 to 16): the pair with the least time for
-// the fullest SM. A warp costs its chunks and about three chunks' time for its start and the joins; an SM's warps share it, but
-// fewer than twelve cannot use it up. Small CTAs lose less at their joins; with few long rows 8 warps in at most 16 CTAs put
-// more warps to work (3 x 8 rows of 40001 slots: 16 x 4 warps 67 us, 12 x 8 warps 47 us).
+// Warps of a CTA (4 or 8) and CTAs that share a (sequence, key/value head, head block): the pair with the least estimated time. A
+// warp costs its chunks and about three chunks' time for its start and the joins; the warps of an SM share it, but fewer than
+// ten cannot use it up; 16 fit, and clusters leave a tenth of the SMs empty (of 16 CTAs: a quarter). Clusters of 11 to 15
+// CTAs are left out: their CTAs come to share SMs while others stay idle. Measured, warps x CTAs: 1024 rows of 1024 slots: 4 x 1
+// 53 us, 4 x 2 66, 8 x 1 59; 24 of 40001: 8 x 10 54, 8 x 12 68, 4 x 10 58, 4 x 16 66, 8 x 1 239; 32 of 1024: 8 x 4 11, 4 x 1 17.
 struct Q4Plan { int warps, ctas; };
 Q4Plan q4_plan(int64_t units, int chunks, int sms) {
   Q4Plan best{4, 1};
   int64_t least = INT64_MAX;
-  for (int warps = 4; warps <= 8; warps += 4)
-    for (int n = 1; n <= 16; ++n) {
-      const int64_t on_sm = (units * n + sms - 1) / sms * warps, each = (chunks + warps * n - 1) / (warps * n) + 3;
-      const int64_t cost = std::max<int64_t>(on_sm, 12) * each;
+  for (int n = 1; n <= 16; n = n == 10 ? 16 : n + 1)
+    for (int warps = 4; warps <= 8; warps += 4) {
+      const int64_t used = n == 1 ? sms : n <= 10 ? sms * 9 / 10 : sms * 3 / 4, places = used * 16 / warps;
+      const int64_t waves = (units * n + places - 1) / places;
+      const int64_t on_sm = waves > 1 ? 16 : std::max<int64_t>((units * n + used - 1) / used * warps, 10);
+      const int64_t cost = waves * on_sm * ((chunks + warps * n - 1) / (warps * n) + 3);
       if (cost < least) { least = cost; best = Q4Plan{warps, n}; }
     }
   return best;

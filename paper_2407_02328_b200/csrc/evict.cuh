@@ -28,7 +28,8 @@ __device__ __forceinline__ int block_sum(int v, int* slots) {
 // contiguous stretch of the row; up to KEYS keys a lane stay in registers for all passes, longer rows are read again. Slots are
 // then handed out in ascending position by ballots, with one sum over the warps before.
 // (Counting needs no atomics: the weights' exponents crowd into few bins of a histogram. Rows of 20001 tokens 57 -> 36 us, 512
-// rows of 512 24 -> 13 us; moving the last candidates to a list that one warp finishes changed neither.)
+// rows of 512 24 -> 13 us; moving the last candidates to a list that one warp finishes changed neither, and a cluster of 8 CTAs per
+// row spent more on its barriers, 63 us.)
 template <int THREADS, int KEYS>
 __global__ void __launch_bounds__(THREADS) evict_select_kernel(const int* seq_start, int total, int Hk, int C, int recent, const float* acc,
                                                                int* slot_pos, float* slot_acc, int* length, unsigned* err) {

@@ -119,11 +119,11 @@ bool allow_smem(size_t bytes, bool wide = false) {
 
 template <typename T, int DH>
 adore_status_t attention_simt(const PackedParams& p, const void* q, const void* k, const void* v, void* out, float* lse, cudaStream_t st) {
-  // Clusters of 4 (2) CTAs per tile while half (all) of the tiles' single CTAs are resident at once; beyond that the tiles
-  // themselves keep the SMs busy and the joins only cost. 8 heads of 64, one prompt of 1024: 1, 2, 4 CTAs 105, 72, 55 us;
-  // 16 heads of 64, 8 prompts of 1024: 519, 570, 665 us.
+  // Clusters of 2 (4, 8) CTAs per tile while the tiles' single CTAs (twice, 16/3 times as many) are resident at once; beyond
+  // that the tiles themselves keep the SMs busy and the joins only cost. 8 heads of 64, one prompt of 1024: 1, 2, 4, 8 CTAs 105,
+  // 72, 55, 64 us; 2 heads of 128, one of 1500: 4, 8 CTAs 131, 71 us; 16 heads of 64, 8 of 1024: 1, 2, 4 CTAs 519, 570, 665 us.
   const int64_t tiles = (int64_t(p.total) / kPsBlock + p.S) * p.H, resident = int64_t(sm_count()) * (DH == 64 ? 4 : 2);
-  const int split = 2 * tiles <= resident ? 4 : tiles <= resident ? 2 : 1;
+  const int split = 16 * tiles <= 3 * resident ? 8 : 2 * tiles <= resident ? 4 : tiles <= resident ? 2 : 1;
   if (tiles * split > kMaxGrid) return ADORE_ERR_UNSUPPORTED;
   if (!allow_smem<prompt_attention_simt_kernel<T, DH>>(prompt_simt_smem<DH>())) return ADORE_ERR_CUDA;
   cudaLaunchConfig_t lc{};

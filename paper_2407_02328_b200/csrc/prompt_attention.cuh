@@ -3,7 +3,7 @@
 //   s_ij = scale q_i . k_j (j <= i),  lse_i = log sum_j exp s_ij,  out_i = sum_j exp(s_ij - lse_i) v_j
 //   acc_j = sum over a group's heads and the queries i >= j of exp(s_ij - lse_i)
 //
-// Attention: 64 query rows of one head, shared by a cluster of 1, 2 or 4 CTAs that take every second or fourth block of 64 keys
+// Attention: 64 query rows of one head, shared by a cluster of 1, 2, 4 or 8 CTAs that take the blocks of 64 keys in turn
 // (a tile's blocks are one after the other otherwise, and the last tiles of a long prompt set the time when there are few)
 // and join their maxima, sums and outputs through distributed shared memory. 128 threads as 8 x 16, 8 x 4 logits each.
 // Weights: 64 key rows of one key/value head, walking over the blocks of queries. 256 threads as 16 x 16, 4 x 4 logits each.

@@ -399,7 +399,8 @@ adore_status_t adore_cache_sync_status(adore_cache_t *cache);
  * head h uses key/value head h / (n_heads / n_kv_heads). scale multiplies the logits; 0 means 1/sqrt(head_dim).
  *
  * error_word: uint32 DEVICE word or NULL. Inconsistencies that only the device sees are skipped there, never followed,
- * and leave a bit (ADORE_WORD_*) in the word; the caller clears it. */
+ * and leave a bit (ADORE_WORD_*) in the word; the caller clears it. Without a word they go unreported. Outputs may not
+ * overlap inputs or one another. */
 enum { ADORE_WORD_TIMEOUT = 1, ADORE_WORD_BOUNDS = 4 };
 
 /* Packed sequences: row t of q, k, v, out belongs to the sequence s with seq_start[s] <= t < seq_start[s + 1]. Rows

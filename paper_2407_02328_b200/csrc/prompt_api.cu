@@ -36,7 +36,7 @@ bool check_strides(int64_t& row, int64_t& head, int64_t rows, int64_t heads, int
   if (row < 0 || head < 0 || row > kMaxStride || head > kMaxStride || row % per16 != 0 || head % per16 != 0) return false;
   if (row < dh || head < dh) return false;
   // the last element's offset has to fit 63 bits with its bytes
-  if (row * (rows > 0 ? rows - 1 : 0) > (int64_t(1) << 58) || head * (heads - 1) > (int64_t(1) << 58)) return false;
+  if (row > (int64_t(1) << 58) / std::max<int64_t>(rows, 1) || head > (int64_t(1) << 58) / heads) return false;
   if (written && rows > 1 && heads > 1) {
     const bool rows_inner = row < head;
     if (rows_inner ? head < row * (rows - 1) + dh : row < head * (heads - 1) + dh) return false;

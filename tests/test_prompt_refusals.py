@@ -30,7 +30,7 @@ BAD_PROMPTS = [
     (dict(struct_size=4), 1), (dict(dtype=2), 1), (dict(n_seqs=0), 1), (dict(total=-1), 1), (dict(n_heads=0), 1), (dict(n_kv_heads=0), 1),
     (dict(n_kv_heads=3), 1), (dict(head_dim=0), 1), (dict(head_dim=96), 8), (dict(head_dim=256), 8), (dict(scale=float("nan")), 1),
     (dict(scale=float("inf")), 1), (dict(q_row=1028), 1), (dict(k_head=4), 1), (dict(k_row=0), 1), (dict(q_head=-128), 1),
-    (dict(q_head=64), 1), (dict(q_row=1 << 40), 1), (dict(dtype=0, q_row=1026), 1),
+    (dict(q_head=64), 1), (dict(total=0x7fff0001), 8), (dict(total=0x7fff0000, k_row=1 << 38), 1), (dict(q_row=1 << 40), 1), (dict(dtype=0, q_row=1026), 1),
 ]
 
 

@@ -6,24 +6,25 @@
 // CTA holds them as the A operand, so that S = K Q^T has a key per TMEM lane and the sum over the queries runs along the
 // columns of one thread: no exchange between threads, no atomics, the same bits every time. Bound by the exponentials: 16 per
 // cycle and SM against 32 logits per cycle from the tensor core (dh = 128).
-// Roles (11 warps, one persistent CTA per SM):
-//   warp 8     producer: looks up the work, loads K tiles (two, the next piece's early) and streams Q tiles by TMA
-//   warp 9     issues S = K Q^T into one of four TMEM buffers of 128 columns
-//   warp 10    stages -lse log2(e) of the item's 128 queries in shared memory
-//   warps 0-7  two warpgroups that take alternate items: S from TMEM, weights, sums (float32 in an item, float64 over items)
+// Roles (19 warps, one persistent CTA per SM):
+//   warps 0-15 four warpgroups that take the items in turn: S from TMEM, weights, sums (float32 in an item, float64 over items)
+//   warp 16    producer: looks up the work, loads K tiles (two, the next piece's early) and streams Q tiles by TMA
+//   warp 17    issues S = K Q^T into one of four TMEM buffers of 128 columns
+//   warp 18    stages -lse log2(e) of the item's 128 queries in shared memory
 #pragma once
 
 #include "prompt_attention_tc.cuh"
 
 namespace adore {
 
-constexpr int kPwThreads = 352;
+constexpr int kPwGroups = 4;              // warpgroups; item i belongs to group and buffer i % 4
+constexpr int kPwThreads = 128 * kPwGroups + 96;
 
 template <int DH>
 struct PwSmem {
   static constexpr int kStages = DH == 128 ? 4 : 6;
   static constexpr int kTileBytes = kPtTile * DH * 2;
-  static constexpr size_t kTotal = size_t(2 + kStages) * kTileBytes + 4 * kPtTile * sizeof(float) + kPtTile * sizeof(double) + 512 + 1024;
+  static constexpr size_t kTotal = size_t(2 + kStages) * kTileBytes + 4 * kPtTile * sizeof(float) + (kPwGroups - 1) * kPtTile * sizeof(double) + 512 + 1024;
 };
 
 struct PwMaps { CUtensorMap q, k; };
@@ -69,8 +70,8 @@ prompt_weights_tc_kernel(const __grid_constant__ PwMaps maps, const PackedParams
   unsigned char* k_tiles = base;
   unsigned char* ring = base + 2 * S::kTileBytes;
   float* offs = reinterpret_cast<float*>(ring + size_t(kStages) * S::kTileBytes);      // [4][128]
-  double* partial = reinterpret_cast<double*>(offs + 4 * kPtTile);                     // [128] second warpgroup's sums
-  uint64_t* q_full = reinterpret_cast<uint64_t*>(partial + kPtTile);
+  double* partial = reinterpret_cast<double*>(offs + 4 * kPtTile);                     // [3][128] the other warpgroups' sums
+  uint64_t* q_full = reinterpret_cast<uint64_t*>(partial + (kPwGroups - 1) * kPtTile);
   uint64_t* q_empty = q_full + kStages;
   uint64_t* k_full = q_empty + kStages;       // [2]
   uint64_t* k_empty = k_full + 2;             // [2] last product with the tile done
@@ -79,7 +80,7 @@ prompt_weights_tc_kernel(const __grid_constant__ PwMaps maps, const PackedParams
   uint64_t* item_empty = l_full + 4;          // [4] buffer and lse slot have been read
   uint64_t* work_full = item_empty + 4;       // [2]
   uint64_t* work_empty = work_full + 2;       // [2]
-  uint64_t* part_full = work_empty + 2;       // the second warpgroup's sums are there / have been read
+  uint64_t* part_full = work_empty + 2;       // the other warpgroups' sums are there / have been read
   uint64_t* part_empty = part_full + 1;
   uint64_t* drain = part_empty + 1;
   __shared__ PwWork works[2];
@@ -87,6 +88,7 @@ prompt_weights_tc_kernel(const __grid_constant__ PwMaps maps, const PackedParams
   __shared__ uint32_t tmem_slot;
   volatile int* abort_flag = &s_abort;
 
+  constexpr int kPwIssuer = 4 * kPwGroups + 1;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     for (uint32_t i = 0; i < kStages; ++i) { tc_mbar_init(&q_full[i], 1u); tc_mbar_init(&q_empty[i], 1u); }
@@ -94,17 +96,17 @@ prompt_weights_tc_kernel(const __grid_constant__ PwMaps maps, const PackedParams
       tc_mbar_init(&k_full[i], 1u);
       tc_mbar_init(&k_empty[i], 1u);
       tc_mbar_init(&work_full[i], 1u);
-      tc_mbar_init(&work_empty[i], 10u);
+      tc_mbar_init(&work_empty[i], 4u * kPwGroups + 2u);
     }
     for (int i = 0; i < 4; ++i) { tc_mbar_init(&s_full[i], 1u); tc_mbar_init(&l_full[i], 1u); tc_mbar_init(&item_empty[i], 4u); }
-    tc_mbar_init(part_full, 4u);
+    tc_mbar_init(part_full, 4u * (kPwGroups - 1));
     tc_mbar_init(part_empty, 4u);
     tc_mbar_init(drain, 1u);
     s_abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
-  if (warp == 9) { __syncwarp(); tc_alloc(&tmem_slot, 512); }
+  if (warp == kPwIssuer) { __syncwarp(); tc_alloc(&tmem_slot, 512); }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -120,7 +122,7 @@ prompt_weights_tc_kernel(const __grid_constant__ PwMaps maps, const PackedParams
     return true;
   };
 
-  if (warp == 8) {
+  if (warp == kPwIssuer - 1) {
     // ---------------- producer ----------------
     bool ok = true;
     PwWork w{};
@@ -157,7 +159,7 @@ prompt_weights_tc_kernel(const __grid_constant__ PwMaps maps, const PackedParams
       }
     }
     if (!ok && lane == 0) give_up();
-  } else if (warp == 9) {
+  } else if (warp == kPwIssuer) {
     // ---------------- MMA issuer ----------------
     constexpr uint32_t idesc = tc_idesc(kPtTile, kPtTile);
     bool ok = true;
@@ -192,7 +194,7 @@ prompt_weights_tc_kernel(const __grid_constant__ PwMaps maps, const PackedParams
       int never = 0;
       tc_mbar_poll_warp(drain, 0u, &never);
     }
-  } else if (warp == 10) {
+  } else if (warp == kPwIssuer + 1) {
     // ---------------- lse of every item's queries ----------------
     bool ok = true;
     uint32_t item = 0;
@@ -218,7 +220,7 @@ prompt_weights_tc_kernel(const __grid_constant__ PwMaps maps, const PackedParams
     }
     if (!ok && lane == 0) give_up();
   } else {
-    // ---------------- weights and sums: warpgroup `group_no` takes every second item, one key per thread ----------------
+    // ---------------- weights and sums: warpgroup `group_no` takes every fourth item, one key per thread ----------------
     const int group_no = warp >> 2, r = threadIdx.x & 127;
     const uint32_t lanes = uint32_t((warp & 3) * 32) << 16;
     const float c = p.scale * 1.4426950408889634f;
@@ -237,7 +239,7 @@ prompt_weights_tc_kernel(const __grid_constant__ PwMaps maps, const PackedParams
         const int q0 = qb * kPtTile;
         const bool masked = qb == w.kb || q0 < first || (last_partial && qb == w.blocks - 1);
         if (++qb == w.blocks) qb = w.qb;
-        if (int(item & 1u) != group_no) continue;
+        if (int(item % kPwGroups) != group_no) continue;
         const uint32_t b = item & 3u, s_at = tmem + lanes + 128 * b;
         const float* off = offs + b * kPtTile;
         if (!tc_mbar_poll_warp(&l_full[b], (item >> 2) & 1u, abort_flag) || !tc_mbar_poll_warp(&s_full[b], (item >> 2) & 1u, abort_flag)) {
@@ -247,15 +249,13 @@ prompt_weights_tc_kernel(const __grid_constant__ PwMaps maps, const PackedParams
         tc_fence_after();
         const int lo = max(q0 == w.kb * kPtTile ? r : 0, first - q0), hi = w.len - q0;
         float part[4];
-        uint32_t s[2][32];
-        __syncwarp();
-        tc_ld_32x32_start(s_at, s[0]);
-        tc_ld_wait(s[0]);
 #pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          if (x < 3) tc_ld_32x32_start(s_at + 32 * (x + 1), s[(x + 1) & 1]);
-          part[x] = masked ? pw_sum32<true>(s[x & 1], off + 32 * x, c, 32 * x, lo, hi) : pw_sum32<false>(s[x & 1], off + 32 * x, c, 0, 0, 0);
-          if (x < 3) tc_ld_wait(s[(x + 1) & 1]);
+        for (int x = 0; x < 4; ++x) {         // the other warps of the SM quarter work during the loads
+          uint32_t s[32];
+          __syncwarp();
+          tc_ld_32x32_start(s_at + 32 * x, s);
+          tc_ld_wait(s);
+          part[x] = masked ? pw_sum32<true>(s, off + 32 * x, c, 32 * x, lo, hi) : pw_sum32<false>(s, off + 32 * x, c, 0, 0, 0);
         }
         tc_fence_before();
         __syncwarp();
@@ -263,15 +263,16 @@ prompt_weights_tc_kernel(const __grid_constant__ PwMaps maps, const PackedParams
         sum += double((part[0] + part[1]) + (part[2] + part[3]));
       }
       if (!ok) break;
-      // the second warpgroup hands its sums over
-      if (group_no == 1) {
+      // the other warpgroups hand their sums over
+      if (group_no > 0) {
         if (it > 0 && !tc_mbar_poll_warp(part_empty, (it - 1) & 1u, abort_flag)) { ok = false; break; }
-        partial[r] = sum;
+        partial[(group_no - 1) * kPtTile + r] = sum;
         __syncwarp();
         if (lane == 0) tc_mbar_arrive(part_full);
       } else {
         if (!tc_mbar_poll_warp(part_full, it & 1u, abort_flag)) { ok = false; break; }
-        const float total = float(sum + partial[r]);
+        for (int x = 0; x < kPwGroups - 1; ++x) sum += partial[x * kPtTile + r];
+        const float total = float(sum);
         __syncwarp();
         if (lane == 0) tc_mbar_arrive(part_empty);
         if (w.kb * kPtTile + r < w.len) acc[size_t(w.g) * p.total + w.start + w.kb * kPtTile + r] = total;
@@ -283,7 +284,7 @@ prompt_weights_tc_kernel(const __grid_constant__ PwMaps maps, const PackedParams
   tc_fence_before();
   __syncthreads();
   if (*abort_flag) {                          // copies in flight have to land before the CTA ends
-    if (warp == 8) {
+    if (warp == kPwIssuer - 1) {
       int never = 0;
       for (uint32_t i = q_issued > kStages ? q_issued - kStages : 0u; i < q_issued; ++i) tc_mbar_poll(&q_full[i % kStages], (i / kStages) & 1u, &never);
       for (uint32_t i = k_issued > 2 ? k_issued - 2 : 0u; i < k_issued; ++i) tc_mbar_poll(&k_full[i & 1u], (i >> 1) & 1u, &never);
@@ -291,7 +292,7 @@ prompt_weights_tc_kernel(const __grid_constant__ PwMaps maps, const PackedParams
     __syncthreads();
   }
   tc_fence_after();
-  if (warp == 9) { __syncwarp(); tc_dealloc(tmem, 512); }
+  if (warp == kPwIssuer) { __syncwarp(); tc_dealloc(tmem, 512); }
 }
 
 }  // namespace adore

@@ -117,7 +117,7 @@ bool allow_smem(size_t bytes, bool wide = false) {
   return true;
 }
 
-template <typename T, int DH>
+template <int DH>
 adore_status_t attention_simt(const PackedParams& p, const void* q, const void* k, const void* v, void* out, float* lse, cudaStream_t st) {
   // Clusters of 2 (4, 8) CTAs per tile while the tiles' single CTAs (twice, 16/3 times as many) are resident at once; beyond
   // that the tiles themselves keep the SMs busy and the joins only cost. 8 heads of 64, one prompt of 1024: 1, 2, 4, 8 CTAs 105,
@@ -125,26 +125,26 @@ adore_status_t attention_simt(const PackedParams& p, const void* q, const void* 
   const int64_t tiles = (int64_t(p.total) / kPsBlock + p.S) * p.H, resident = int64_t(sm_count()) * (DH == 64 ? 4 : 2);
   const int split = 16 * tiles <= 3 * resident ? 8 : 2 * tiles <= resident ? 4 : tiles <= resident ? 2 : 1;
   if (tiles * split > kMaxGrid) return ADORE_ERR_UNSUPPORTED;
-  if (!allow_smem<prompt_attention_simt_kernel<T, DH>>(prompt_simt_smem<DH>())) return ADORE_ERR_CUDA;
+  if (!allow_smem<prompt_attention_simt_kernel<DH>>(prompt_simt_smem<DH>())) return ADORE_ERR_CUDA;
   cudaLaunchConfig_t lc{};
   cudaLaunchAttribute at[1];
   at[0].id = cudaLaunchAttributeClusterDimension;
   at[0].val.clusterDim.x = unsigned(split); at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
   lc.gridDim = dim3(unsigned(tiles * split)); lc.blockDim = dim3(kPaThreads); lc.dynamicSmemBytes = prompt_simt_smem<DH>(); lc.stream = st;
   lc.attrs = at; lc.numAttrs = split > 1 ? 1 : 0;
-  const cudaError_t e = cudaLaunchKernelEx(&lc, prompt_attention_simt_kernel<T, DH>, p, split, static_cast<const T*>(q),
-                                           static_cast<const T*>(k), static_cast<const T*>(v), static_cast<T*>(out), lse);
+  const cudaError_t e = cudaLaunchKernelEx(&lc, prompt_attention_simt_kernel<DH>, p, split, static_cast<const float*>(q),
+                                           static_cast<const float*>(k), static_cast<const float*>(v), static_cast<float*>(out), lse);
   if (e != cudaSuccess) { cudaGetLastError(); return ADORE_ERR_CUDA; }
   return launched();
 }
 
-template <typename T, int DH>
+template <int DH>
 adore_status_t weights_simt(const PackedParams& p, const void* q, const void* k, const float* lse, int window, float* acc, cudaStream_t st) {
   const unsigned grid = tile_grid(p, kPsBlock, p.Hk);
   if (grid == 0) return ADORE_ERR_UNSUPPORTED;
-  if (!allow_smem<prompt_weights_simt_kernel<T, DH>>(prompt_weights_simt_smem<DH>())) return ADORE_ERR_CUDA;
-  prompt_weights_simt_kernel<T, DH><<<grid, kPsThreads, prompt_weights_simt_smem<DH>(), st>>>(
-      p, static_cast<const T*>(q), static_cast<const T*>(k), lse, window, acc);
+  if (!allow_smem<prompt_weights_simt_kernel<DH>>(prompt_weights_simt_smem<DH>())) return ADORE_ERR_CUDA;
+  prompt_weights_simt_kernel<DH><<<grid, kPsThreads, prompt_weights_simt_smem<DH>(), st>>>(
+      p, static_cast<const float*>(q), static_cast<const float*>(k), lse, window, acc);
   return launched();
 }
 
@@ -312,7 +312,7 @@ adore_status_t adore_prompt_attention(const adore_prompt_t* shape, const int32_t
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   if (shape->dtype == ADORE_BF16)
     return shape->head_dim == 64 ? attention_tc<64>(p, q, k, v, out, lse, st) : attention_tc<128>(p, q, k, v, out, lse, st);
-  return shape->head_dim == 64 ? attention_simt<float, 64>(p, q, k, v, out, lse, st) : attention_simt<float, 128>(p, q, k, v, out, lse, st);
+  return shape->head_dim == 64 ? attention_simt<64>(p, q, k, v, out, lse, st) : attention_simt<128>(p, q, k, v, out, lse, st);
 }
 
 adore_status_t adore_prompt_weights(const adore_prompt_t* shape, const int32_t* seq_start, const void* q, const void* k,
@@ -326,8 +326,8 @@ adore_status_t adore_prompt_weights(const adore_prompt_t* shape, const int32_t* 
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   if (shape->dtype == ADORE_BF16)
     return shape->head_dim == 64 ? weights_tc<64>(p, q, k, lse, window, acc, st) : weights_tc<128>(p, q, k, lse, window, acc, st);
-  return shape->head_dim == 64 ? weights_simt<float, 64>(p, q, k, lse, window, acc, st)
-                               : weights_simt<float, 128>(p, q, k, lse, window, acc, st);
+  return shape->head_dim == 64 ? weights_simt<64>(p, q, k, lse, window, acc, st)
+                               : weights_simt<128>(p, q, k, lse, window, acc, st);
 }
 
 size_t adore_q4_bytes(const adore_q4_t* shape) {

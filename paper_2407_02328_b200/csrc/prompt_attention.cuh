@@ -29,8 +29,8 @@ template <int DH>
 constexpr size_t prompt_weights_simt_smem() { return size_t(2 * DH * kPsPitch + kPsBlock) * sizeof(float); }
 
 // 64 rows from `row0` of a sequence of `len` rows, transposed to dst[e][row]; lanes of a warp take 8 rows x 4 pieces.
-template <typename T, int DH>
-__device__ __forceinline__ void load_transposed(float* dst, const T* src, long long row_stride, int row0, int len) {
+template <int DH>
+__device__ __forceinline__ void load_transposed(float* dst, const float* src, long long row_stride, int row0, int len) {
   for (int i = threadIdx.x; i < kPsBlock * (DH / 4); i += blockDim.x) {
     const int low = i & 31, r = (low & 7) + 8 * ((i >> 5) & 7), c = (low >> 3) + 4 * (i >> 8);
     float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -63,9 +63,9 @@ __device__ __forceinline__ void tile_product(const float* a, const float* b, int
   }
 }
 
-template <typename T, int DH>
-__global__ void __launch_bounds__(kPaThreads, DH == 64 ? 4 : 2) prompt_attention_simt_kernel(const PackedParams p, int split, const T* q,
-                                                                                            const T* k, const T* v, T* out, float* lse) {
+template <int DH>
+__global__ void __launch_bounds__(kPaThreads, DH == 64 ? 4 : 2) prompt_attention_simt_kernel(const PackedParams p, int split, const float* q,
+                                                                                            const float* k, const float* v, float* out, float* lse) {
   extern __shared__ __align__(16) float prompt_smem[];
   float* qt = prompt_smem;
   float* kt = qt + DH * kPsPitch;          // later the weights of the block, transposed
@@ -84,10 +84,10 @@ __global__ void __launch_bounds__(kPaThreads, DH == 64 ? 4 : 2) prompt_attention
   if (!found) return;                      // alike in all CTAs of the cluster
   const int len = tile.len, q0 = tile.index * kPsBlock;
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  const T* qs = q + tile.start * p.q_row + h * p.q_head;
-  const T* ks = k + tile.start * p.k_row + g * p.k_head;
-  const T* vsrc = v + tile.start * p.v_row + g * p.v_head;
-  load_transposed<T, DH>(qt, qs, p.q_row, q0, len);
+  const float* qs = q + tile.start * p.q_row + h * p.q_head;
+  const float* ks = k + tile.start * p.k_row + g * p.k_head;
+  const float* vsrc = v + tile.start * p.v_row + g * p.v_head;
+  load_transposed<DH>(qt, qs, p.q_row, q0, len);
   constexpr int R = 8, NV = DH / 64;       // rows of a thread, 16-byte pieces of a value row per thread
   float o[R][4 * NV], m[R], l[R];
 #pragma unroll
@@ -100,7 +100,7 @@ __global__ void __launch_bounds__(kPaThreads, DH == 64 ? 4 : 2) prompt_attention
   const float c = p.scale * 1.4426950408889634f;      // logits in units of log 2
   for (int kb = rank; kb <= tile.index; kb += split) {
     __syncthreads();
-    load_transposed<T, DH>(kt, ks, p.k_row, kb * kPsBlock, len);
+    load_transposed<DH>(kt, ks, p.k_row, kb * kPsBlock, len);
     for (int i = threadIdx.x; i < kPsBlock * (DH / 4); i += kPaThreads) {
       const int r = i / (DH / 4), e = i % (DH / 4);
       float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -168,7 +168,7 @@ __global__ void __launch_bounds__(kPaThreads, DH == 64 ? 4 : 2) prompt_attention
       const int r = q0 + R * ty + i;
       if (r >= len) continue;
       const float inv = 1.f / l[i];
-      T* dst = out + (tile.start + r) * p.out_row + h * p.out_head;
+      float* dst = out + (tile.start + r) * p.out_row + h * p.out_head;
 #pragma unroll
       for (int n = 0; n < NV; ++n)
         store4(dst + 64 * n + 4 * tx, make_float4(o[i][4 * n] * inv, o[i][4 * n + 1] * inv, o[i][4 * n + 2] * inv, o[i][4 * n + 3] * inv));
@@ -209,8 +209,8 @@ __global__ void __launch_bounds__(kPaThreads, DH == 64 ? 4 : 2) prompt_attention
   cluster.sync();                          // nobody leaves while its shared memory is read
 }
 
-template <typename T, int DH>
-__global__ void __launch_bounds__(kPsThreads, 2) prompt_weights_simt_kernel(const PackedParams p, const T* q, const T* k,
+template <int DH>
+__global__ void __launch_bounds__(kPsThreads, 2) prompt_weights_simt_kernel(const PackedParams p, const float* q, const float* k,
                                                                             const float* lse, int window, float* acc) {
   extern __shared__ __align__(16) float prompt_smem[];
   float* kt = prompt_smem;
@@ -230,7 +230,7 @@ __global__ void __launch_bounds__(kPsThreads, 2) prompt_weights_simt_kernel(cons
   const int kb = blocks - 1 - tile.index, k0 = kb * kPsBlock;      // early keys are seen by most queries
   const int first = window > 0 ? max(0, len - window) : 0;         // first query that counts
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  load_transposed<T, DH>(kt, k + tile.start * p.k_row + g * p.k_head, p.k_row, k0, len);
+  load_transposed<DH>(kt, k + tile.start * p.k_row + g * p.k_head, p.k_row, k0, len);
   const float c = p.scale * 1.4426950408889634f;
   float sum[4] = {0.f, 0.f, 0.f, 0.f};
   for (int h = g * p.group; h < (g + 1) * p.group; ++h) {
@@ -238,7 +238,7 @@ __global__ void __launch_bounds__(kPsThreads, 2) prompt_weights_simt_kernel(cons
     for (int qb = max(kb, first / kPsBlock); qb < blocks; ++qb) {
       const int q0 = qb * kPsBlock;
       __syncthreads();
-      load_transposed<T, DH>(qt, q + tile.start * p.q_row + h * p.q_head, p.q_row, q0, len);
+      load_transposed<DH>(qt, q + tile.start * p.q_row + h * p.q_head, p.q_row, q0, len);
       if (threadIdx.x < kPsBlock) {
         const int i = q0 + threadIdx.x;
         ls[threadIdx.x] = i >= first && i < len ? lrow[i] * 1.4426950408889634f : INFINITY;    // infinite: weight 0

@@ -153,3 +153,13 @@ def test_the_binding_refuses_tensors_that_do_not_fit(lib):
         with pytest.raises(lib.AdoreError) as e:
             call()
         assert e.value.status == 1
+
+
+@pytest.mark.parametrize("shape", [dict(batch=65536, n_heads=1, n_kv_heads=1), dict(batch=1, n_heads=65536, n_kv_heads=65536)])
+def test_rows_beyond_a_grids_dimensions(lib, shape):
+    """Fills and reads refuse what their grids cannot hold, before the selection has written anything."""
+    l, c = lib._lib(), _q4(lib, **shape)
+    row = 128 * c.n_kv_heads
+    p = _prompt(lib, n_seqs=c.batch, n_heads=c.n_heads, n_kv_heads=c.n_kv_heads, k_row=row, v_row=row)
+    assert l.adore_evict_prompt(C.byref(c), C.byref(p), A, A, A, A, 1, A, A, A, A, None, None) == 8
+    assert l.adore_q4_read(C.byref(c), A, A, 1, A, A, None) == 8
